@@ -18,6 +18,8 @@ Diffusion Large Language Models):
   entropy.row_entropy, tail_entropy_scores, select_start_block
                                Sec. "Training-Free MBE Decoding", tail-entropy
                                block selection, Eqs. (5)-(6).
+  q8.*                         the 8-bit cache (types, quantising write, read-back)
+                               and the rotation of queries and keys.
   kv_cache.kv_write, refresh_blocks
                                Sec. "Infrastructure Optimization", cache
                                control: write-back of recomputed K/V.

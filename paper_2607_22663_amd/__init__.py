@@ -8,11 +8,19 @@ cannot be loaded, every call raises; there is no other implementation.
     window_attention(q, k_pages, v_pages, page_table, prefix_lens, window_lens, block_size)
     block_diffusion_attention(q, k_pages, v_pages, page_table, prefix_lens, block_size)
     edit_select(logits, cur_tokens, threshold) -> (new_tokens, conf, changed_mask)
+
+The 8-bit KV cache (include/mbe_q8.h), from a layer's projections to its output:
+
+    rotary(q, k, start_pos, lens, turns) -> (q, k)
+    kv_write_q8(k_pages, v_pages, k_scales, v_scales, page_table, start_pos, lens, k_new, v_new)
+    window_attention_q8(q, k_pages, v_pages, k_scales, v_scales, page_table, prefix_lens, window_lens, block_size)
+    kv_read_q8(k_pages, v_pages, k_scales, v_scales, page_table, start_pos, lens) -> (k, v)
 """
 from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 import threading
 from typing import Optional
@@ -31,6 +39,10 @@ EXPORTS = ("mbe_window_attention", "block_diffusion_attention", "mbe_window_atte
            "mbe_threshold_update", "mbe_threshold_update_workspace_size", "mbe_tail_entropy_scores",
            "mbe_select_start_block", "mbe_kv_write", "mbe_refresh_blocks", "mbe_status_string", "mbe_last_error",
            "mbe_threshold_update_noalloc", "mbe_window_attention_plan")
+EXPORTS_Q8 = ("mbe_kv_write_q8", "mbe_kv_read_q8", "mbe_window_attention_q8",
+              "mbe_window_attention_q8_workspace_size", "mbe_rotary")
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+Q8_FORMATS = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
 ACTIONS = {"keep": 0, "unmask": 1, "force_unmask": 2, "edit": 3}
 REFRESH_MODES = {"changed": 0, "changed_and_later": 1}
 
@@ -80,6 +92,12 @@ class AttnPlan(ctypes.Structure):
                 ("pipelined", ctypes.c_int32), ("workgroups", ctypes.c_int64)]
 
 
+class PagedKVQ8(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
 _lib = None
 _lock = threading.Lock()
 
@@ -96,7 +114,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         if not os.path.exists(p):
             raise RuntimeError(f"{p} not found: build it with `python -m paper_2607_22663_amd.build`")
         lib = ctypes.CDLL(p)
-        for name in EXPORTS:
+        for name in EXPORTS + EXPORTS_Q8:
             if not hasattr(lib, name):
                 raise RuntimeError(f"{p} does not export {name}")
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
@@ -134,6 +152,18 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         lib.mbe_kv_write.restype = ctypes.c_int
         lib.mbe_refresh_blocks.argtypes = [vp, i32, i32, i32, vp, vp]
         lib.mbe_refresh_blocks.restype = ctypes.c_int
+        q8 = ctypes.POINTER(PagedKVQ8)
+        lib.mbe_kv_write_q8.argtypes = [q8, vp, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, i32, vp]
+        lib.mbe_kv_write_q8.restype = ctypes.c_int
+        lib.mbe_kv_read_q8.argtypes = [q8, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp]
+        lib.mbe_kv_read_q8.restype = ctypes.c_int
+        lib.mbe_window_attention_q8.argtypes = [vp, q8, vp, vp, vp, i32, vp, ctypes.POINTER(AttnOpts)]
+        lib.mbe_window_attention_q8.restype = ctypes.c_int
+        lib.mbe_window_attention_q8_workspace_size.argtypes = [q8, ctypes.POINTER(AttnOpts)]
+        lib.mbe_window_attention_q8_workspace_size.restype = sz
+        lib.mbe_rotary.argtypes = [vp, vp, i32, i64, i64, vp, vp, i32, i64, i64, i32, vp, vp, i32, i32, i32, vp, i32,
+                                   i32, f32, i32, vp]
+        lib.mbe_rotary.restype = ctypes.c_int
         lib.mbe_status_string.argtypes = [ctypes.c_int]
         lib.mbe_status_string.restype = ctypes.c_char_p
         lib.mbe_last_error.argtypes = []
@@ -222,7 +252,7 @@ def _workspace(kind: str, device: torch.device, nbytes: int) -> Optional[torch.T
 MBE_ERR_WORKSPACE = 4
 
 
-def _call_with_workspace(call, size, opts, device, workspace):
+def _call_with_workspace(call, size, opts, device, workspace, kind="attn"):
     """Runs an attention call whose split plan may need a workspace.  With a
     caller's workspace, that one.  Otherwise the shared workspace of this
     stream as it is, first: only when the library reports it too small (or
@@ -233,7 +263,7 @@ def _call_with_workspace(call, size, opts, device, workspace):
             raise ValueError("workspace must be a uint8 device tensor")
         opts.workspace, opts.workspace_bytes = _ptr(workspace), workspace.numel()
         return call()
-    key = ("attn", device.index, opts.stream or 0)
+    key = (kind, device.index, opts.stream or 0)
     ws = _workspaces.get(key)
     opts.workspace, opts.workspace_bytes = (_ptr(ws), ws.numel()) if ws is not None else (None, 0)
     status = call()
@@ -242,7 +272,7 @@ def _call_with_workspace(call, size, opts, device, workspace):
     need = size()
     if need == ctypes.c_size_t(-1).value:
         return status
-    ws = _workspace("attn", device, need)
+    ws = _workspace(kind, device, need)
     opts.workspace, opts.workspace_bytes = (_ptr(ws), need) if ws is not None else (None, 0)
     return call()
 
@@ -633,3 +663,295 @@ def refresh_blocks(block_changed, mode="changed", *, out=None):
         _ptr(block_changed), block_changed.shape[0], block_changed.shape[1], REFRESH_MODES[mode], _ptr(refresh),
         _stream(dev)))
     return refresh
+
+
+# ------------------------------------------------------------ 8-bit KV cache
+def _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table):
+    """The 8-bit pools of a layer as the library's structure, checked."""
+    try:      # the usual case: everything as it should be, in one test
+        index = k_pages.get_device()
+        n_pages, hkv, page, d = k_pages.shape
+        fmt = Q8_FORMATS[k_pages.dtype]
+        usual = (index >= 0 and v_pages.dtype is k_pages.dtype and v_pages.shape == (n_pages, hkv, d, page)
+                 and k_scales.dtype is _F32 and v_scales.dtype is _F32 and page_table.dtype is _I32
+                 and k_scales.shape == (n_pages, hkv) and v_scales.shape == (n_pages, hkv) and page_table.dim() == 2
+                 and v_pages.get_device() == index and k_scales.get_device() == index
+                 and v_scales.get_device() == index and page_table.get_device() == index
+                 and k_pages.is_contiguous() and v_pages.is_contiguous() and k_scales.is_contiguous()
+                 and v_scales.is_contiguous() and page_table.is_contiguous())
+    except (AttributeError, ValueError, KeyError, RuntimeError):
+        usual = False
+    if not usual:
+        _pool_q8_explain(k_pages, v_pages, k_scales, v_scales, page_table)
+        n_pages, hkv, page, d = k_pages.shape
+        fmt = Q8_FORMATS[k_pages.dtype]
+    return PagedKVQ8(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n_pages, page,
+                     hkv, d, fmt)
+
+
+def _pool_q8_explain(k_pages, v_pages, k_scales, v_scales, page_table):
+    """The checks of _pool_q8 one by one: raises for the first that fails."""
+    if not isinstance(k_pages, torch.Tensor):
+        raise TypeError("k_pages must be a torch.Tensor")
+    if k_pages.dtype not in Q8_FORMATS:
+        raise TypeError(f"k_pages must be one of {list(Q8_FORMATS)}, got {k_pages.dtype}")
+    dev = k_pages.device
+    _raw_stream(dev)          # (refuses anything but a GPU)
+    _need(k_pages, "k_pages", k_pages.dtype, dev, 4)
+    _need(v_pages, "v_pages", k_pages.dtype, dev, 4)
+    n_pages, hkv, page, d = k_pages.shape
+    if tuple(v_pages.shape) != (n_pages, hkv, d, page):
+        raise ValueError(f"v_pages must be [num_pages, Hkv, D, 16] = {(n_pages, hkv, d, page)}, got "
+                         f"{tuple(v_pages.shape)}")
+    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+        _need(t, name, _F32, dev, 2)
+        if tuple(t.shape) != (n_pages, hkv):
+            raise ValueError(f"{name} must be [num_pages, Hkv] = {(n_pages, hkv)}, got {tuple(t.shape)}")
+    _need(page_table, "page_table", _I32, dev, 2)
+
+
+def _ranges_q8(kv, page_table, start_pos, lens, max_len):
+    """Checks the ranges of a write or a read; returns (batch, max_len)."""
+    dev = page_table.device
+    _need(start_pos, "start_pos", _I32, dev, 1)
+    _need(lens, "lens", _I32, dev, 1)
+    batch = start_pos.shape[0]
+    if lens.shape[0] != batch or page_table.shape[0] != batch:
+        raise ValueError("page_table, start_pos and lens disagree on the batch size")
+    if max_len is None:
+        max_len = int(lens.max().item()) if batch else 0
+    return batch, int(max_len)
+
+
+@_on_device
+def kv_write_q8(k_pages, v_pages, k_scales, v_scales, page_table, start_pos, lens, k_new, v_new, *, max_len=None,
+                kv_lens=None, block_flags=None, block_size=None):
+    """Quantise K/V (bf16 [total_tokens, Hkv, D]) into 8-bit paged pools in
+    place: token t of sequence b goes to position start_pos[b] + t, and every
+    page it touches gets one power-of-two scale for each head, of K and of V
+    (include/mbe_q8.h has the rule).
+
+    k_pages: float8_e4m3fn or float8_e5m2 [num_pages, Hkv, 16, D]; v_pages: the
+    same type, [num_pages, Hkv, D, 16]; scales: float32 [num_pages, Hkv].
+    kv_lens: optional int32 [batch], the tokens each sequence holds before the
+    call; needed when tokens behind the written range are to be kept (None: the
+    call appends).  max_len: bound of lens (None: read from the device, a
+    synchronisation).  block_flags, block_size: as for kv_write."""
+    lib = load()
+    kv = _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table)
+    dev = k_pages.device
+    batch, max_len = _ranges_q8(kv, page_table, start_pos, lens, max_len)
+    _need(k_new, "k_new", _BF16, dev, 3)
+    _need(v_new, "v_new", _BF16, dev, 3)
+    if k_new.shape != v_new.shape or k_new.shape[1] != kv.num_kv_heads or k_new.shape[2] != kv.head_dim:
+        raise ValueError(f"k_new and v_new must be [total_tokens, {kv.num_kv_heads}, {kv.head_dim}], got "
+                         f"{tuple(k_new.shape)} and {tuple(v_new.shape)}")
+    if kv_lens is not None:
+        _need(kv_lens, "kv_lens", _I32, dev, 1)
+        if kv_lens.shape[0] != batch:
+            raise ValueError("kv_lens must have one entry per sequence")
+    if block_flags is not None:
+        if block_size is None or int(block_size) < 1:
+            raise ValueError("block_flags needs block_size >= 1")
+        _flags_gate(block_flags, (batch, -(-max_len // int(block_size))), None, dev)
+    _check("mbe_kv_write_q8", lib.mbe_kv_write_q8(
+        ctypes.byref(kv), _ptr(page_table), page_table.shape[1], _ptr(start_pos), _ptr(lens), _ptr(kv_lens), batch,
+        max_len, k_new.shape[0], _ptr(k_new), _ptr(v_new), _ptr(block_flags), int(block_size or 0), _stream(dev)))
+
+
+@_on_device
+def kv_read_q8(k_pages, v_pages, k_scales, v_scales, page_table, start_pos, lens, *, max_len=None, total=None,
+               out=None):
+    """Read tokens start_pos[b] .. start_pos[b] + lens[b] - 1 of every sequence
+    back as bf16 [total, Hkv, D] (k, v).  `total` (rows, the sum of lens) and
+    max_len are read from the device when neither they nor `out` say them (a
+    synchronisation).  out: optional (k, v) tensors to write to."""
+    lib = load()
+    kv = _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table)
+    dev = k_pages.device
+    batch, max_len = _ranges_q8(kv, page_table, start_pos, lens, max_len)
+    if out is None:
+        rows = int(lens.sum().item()) if total is None else int(total)
+        out = tuple(torch.empty(rows, kv.num_kv_heads, kv.head_dim, dtype=_BF16, device=dev) for _ in range(2))
+    k, v = out
+    _need(k, "out[0]", _BF16, dev, 3)
+    _need(v, "out[1]", _BF16, dev, 3)
+    if k.shape != v.shape or k.shape[1] != kv.num_kv_heads or k.shape[2] != kv.head_dim:
+        raise ValueError(f"outputs must be [total, {kv.num_kv_heads}, {kv.head_dim}], got {tuple(k.shape)} and "
+                         f"{tuple(v.shape)}")
+    _check("mbe_kv_read_q8", lib.mbe_kv_read_q8(
+        ctypes.byref(kv), _ptr(page_table), page_table.shape[1], _ptr(start_pos), _ptr(lens), batch, max_len,
+        k.shape[0], _ptr(k), _ptr(v), _stream(dev)))
+    return k, v
+
+
+@_on_device
+def window_attention_q8(q, k_pages, v_pages, k_scales, v_scales, page_table, prefix_lens, window_lens, block_size, *,
+                        out=None, mask_mode="bidir", softmax_scale=None, max_prefix_len=None, max_window_len=None,
+                        kv_split_tokens=0, host_prefix_lens=None, host_window_lens=None, workspace=None,
+                        block_flags=None, run_if_nonzero=None):
+    """window_attention over an 8-bit cache (pools and scales as for
+    kv_write_q8); windows of any length, one token included.  The arguments are
+    those of window_attention.  The lengths' bounds are needed on the host
+    (max_prefix_len, max_window_len, or host copies of the lengths; without
+    either the lengths are copied from the device, a synchronisation).  The work
+    is dealt out on the device by the true lengths."""
+    lib = load()
+    kv = _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table)
+    dev = k_pages.device
+    _need(q, "q", _BF16, dev, 3)
+    _need(prefix_lens, "prefix_lens", _I32, dev, 1)
+    _need(window_lens, "window_lens", _I32, dev, 1)
+    if q.shape[2] != kv.head_dim:
+        raise ValueError(f"q head_dim {q.shape[2]} != cache head_dim {kv.head_dim}")
+    batch = prefix_lens.shape[0]
+    if window_lens.shape[0] != batch or page_table.shape[0] != batch:
+        raise ValueError("page_table, prefix_lens and window_lens disagree on the batch size")
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need(out, "out", _BF16, dev, 3)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    if max_prefix_len is None:
+        host = _host_i32(prefix_lens.cpu() if host_prefix_lens is None else host_prefix_lens, batch, "host_prefix_lens")
+        max_prefix_len = int(host.max()) if batch else 0
+    if max_window_len is None:
+        host = _host_i32(window_lens.cpu() if host_window_lens is None else host_window_lens, batch, "host_window_lens")
+        max_window_len = int(host.max()) if batch else 0
+    nblk = int(max_window_len) // int(block_size) if int(block_size) > 0 else 0
+    _flags_gate(block_flags, (batch, nblk), run_if_nonzero, dev)
+    opts = AttnOpts(batch, q.shape[1], page_table.shape[1], q.shape[0], int(max_prefix_len), int(max_window_len),
+                    MASK_MODES[mask_mode] if isinstance(mask_mode, str) else int(mask_mode),
+                    float(softmax_scale or 0.0), int(kv_split_tokens), None, None, None, 0, _stream(dev),
+                    _ptr(block_flags), _ptr(run_if_nonzero))
+
+    def call():
+        return lib.mbe_window_attention_q8(_ptr(q), ctypes.byref(kv), _ptr(page_table), _ptr(prefix_lens),
+                                           _ptr(window_lens), int(block_size), _ptr(out), ctypes.byref(opts))
+
+    def size():
+        return lib.mbe_window_attention_q8_workspace_size(ctypes.byref(kv), ctypes.byref(opts))
+
+    _check("mbe_window_attention_q8", _call_with_workspace(call, size, opts, dev, workspace, "attn_q8"))
+    return out
+
+
+def workspace_bytes_window_attention_q8(q, k_pages, page_table, batch, *, max_prefix_len, max_window_len,
+                                        kv_split_tokens=0):
+    """Workspace bytes of a window_attention_q8 call with these shapes and
+    bounds, for callers that own the workspace (a captured graph)."""
+    kv = PagedKVQ8(None, None, None, None, k_pages.shape[0], k_pages.shape[2], k_pages.shape[1], k_pages.shape[3],
+                   Q8_FORMATS[k_pages.dtype])
+    opts = AttnOpts(int(batch), q.shape[1], page_table.shape[1], q.shape[0], int(max_prefix_len), int(max_window_len),
+                    0, 0.0, int(kv_split_tokens), None, None, None, 0, None, None, None)
+    n = load().mbe_window_attention_q8_workspace_size(ctypes.byref(kv), ctypes.byref(opts))
+    if n == ctypes.c_size_t(-1).value:
+        raise ValueError("invalid attention shapes")
+    return n
+
+
+# ---------------------------------------------------------- rotary positions
+def rotary_frequencies(rot_dim, base=10000.0, *, scaling=None, factor=1.0, original_len=4096, slow_turns=1.0,
+                       fast_turns=32.0):
+    """Radians per position of the rot_dim / 2 pairs, float64 on the host:
+    base ** (-2 i / rot_dim), and for a context `factor` times longer
+      scaling="linear"  every frequency divided by factor (positions
+                        interpolated)
+      scaling="base"    base * factor ** (rot_dim / (rot_dim - 2)): the slowest
+                        frequency divided by factor, the fastest kept
+      scaling="ramp"    frequencies with fewer than slow_turns turns in
+                        original_len positions divided by factor, those with
+                        more than fast_turns kept, a linear ramp in the turns
+                        between them"""
+    half = rot_dim // 2
+    i = torch.arange(half, dtype=torch.float64) / half
+    if scaling == "base":
+        base = base * factor ** (rot_dim / max(rot_dim - 2, 1))
+    f = float(base) ** -i
+    if scaling is None or scaling == "base":
+        return f
+    if scaling == "linear":
+        return f / factor
+    if scaling == "ramp":
+        keep = ((original_len * f / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns)).clamp(0, 1)
+        return f * keep + f / factor * (1 - keep)
+    raise ValueError(f"scaling {scaling!r}: None, 'linear', 'base' or 'ramp'")
+
+
+def rotary_turns(frequencies, device):
+    """The table `rotary` takes: each frequency (radians per position) as turns
+    per position in units of 2^-64, modulo one turn, int64 on the device."""
+    turns = []
+    for f in torch.as_tensor(frequencies, dtype=torch.float64).tolist():
+        t = f / (2 * math.pi)
+        n = int((t - math.floor(t)) * 2.0 ** 64) % (1 << 64)
+        turns.append(n - (1 << 64) if n >= 1 << 63 else n)
+    return torch.tensor(turns, dtype=torch.int64).to(device)
+
+
+def _rows_of(t, name, device, heads_dim):
+    """Row stride of a [rows, heads, D] tensor whose rows are whole but may lie
+    apart (a slice of a packed projection)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != _BF16:
+        raise TypeError(f"{name} must be {_BF16}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have 3 dimensions, got {t.dim()}")
+    rows, heads, d = t.shape
+    if heads_dim is not None and (heads, d) != heads_dim:
+        raise ValueError(f"{name} must be [rows, {heads_dim[0]}, {heads_dim[1]}], got {tuple(t.shape)}")
+    if t.numel() and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d)):
+        raise ValueError(f"{name}: each row's heads must be contiguous")
+    return t.stride(0) if rows > 1 else heads * d
+
+
+@_on_device
+def rotary(q, k, start_pos, lens, turns, *, scale=1.0, layout="half", inverse=False, max_len=None, out=None):
+    """Rotate the heads of q [rows, Hq, D] and k [rows, Hkv, D] (bf16; k may be
+    None) by their positions: row t of sequence b is at start_pos[b] + t.
+    turns: int64 [rot_dim / 2], from rotary_turns; the dims from rot_dim on are
+    copied.  layout "half" pairs dim i with i + rot_dim / 2, "interleaved" 2i
+    with 2i + 1.  scale multiplies the rotated dims.  inverse=True rotates back
+    (the gradient of the call).  Rows may lie apart (slices of one packed
+    projection).  out: optional (q, k) to write to; (q, k) themselves rotate in
+    place.  max_len: bound of lens (None: read from the device, a
+    synchronisation).  Returns (q, k) rotated, k None if it was."""
+    lib = load()
+    dev = q.device
+    q_stride = _rows_of(q, "q", dev, None)
+    rows, hq, d = q.shape
+    hkv, k_stride = 0, 0
+    if k is not None:
+        k_stride = _rows_of(k, "k", dev, None)
+        hkv = k.shape[1]
+        if k.shape[0] != rows or k.shape[2] != d:
+            raise ValueError(f"q and k disagree on rows or head_dim: {tuple(q.shape)} and {tuple(k.shape)}")
+    _need(start_pos, "start_pos", _I32, dev, 1)
+    _need(lens, "lens", _I32, dev, 1)
+    _need(turns, "turns", torch.int64, dev, 1)
+    batch = start_pos.shape[0]
+    if lens.shape[0] != batch:
+        raise ValueError("start_pos and lens disagree on the batch size")
+    stream = _stream(dev)
+    if max_len is None:
+        max_len = int(lens.max().item()) if batch else 0
+    if out is None:
+        q_out = torch.empty(q.shape, dtype=_BF16, device=dev)
+        k_out = None if k is None else torch.empty(k.shape, dtype=_BF16, device=dev)
+    else:
+        q_out, k_out = out
+        if (k is None) != (k_out is None):
+            raise ValueError("out must hold k exactly when k is given")
+    q_out_stride = _rows_of(q_out, "out[0]", dev, (hq, d))
+    k_out_stride = 0 if k is None else _rows_of(k_out, "out[1]", dev, (hkv, d))
+    if q_out.shape[0] != rows or (k is not None and k_out.shape[0] != rows):
+        raise ValueError("outputs must have the rows of the inputs")
+    _check("mbe_rotary", lib.mbe_rotary(
+        _ptr(q), _ptr(q_out), hq, q_stride, q_out_stride, _ptr(k), _ptr(k_out), hkv, k_stride, k_out_stride, d,
+        _ptr(start_pos), _ptr(lens), batch, int(max_len), rows, _ptr(turns), 2 * turns.shape[0],
+        ROTARY_LAYOUTS[layout], float(scale), int(bool(inverse)), stream))
+    return q_out, k_out

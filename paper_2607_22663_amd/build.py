@@ -19,7 +19,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmbe.so")
 TIMELINE_LIB = os.path.join(PKG, "libmbe_timeline.so")
-SOURCES = ["abi.cpp", "edit_select.hip", "attn_window.hip", "block_select.hip", "kv_write.hip", "noalloc.hip"]
+SOURCES = ["abi.cpp", "edit_select.hip", "attn_window.hip", "block_select.hip", "kv_write.hip", "noalloc.hip",
+           "abi_q8.cpp", "kv_q8.hip", "rotary.hip", "attn_q8.hip"]
 
 # Packed fp32 VALU ops are disabled for every HIP source: ordinary float code
 # is compiled to scalar-per-lane v_*_f32 instructions only.  MFMA results are
