@@ -137,8 +137,9 @@ mbe::KvQ8Params range_params(const mbe_paged_kv_q8 *kv, const int32_t *page_tabl
 }
 
 // --------------------------------------------------------------- attention
-// Shares of the work: two workgroups of four waves on each of the 256 CUs.
-constexpr int64_t kStreamWgs = 512;
+// Shares of the work: one workgroup of eight waves, or two of four, on each of
+// the 256 CUs.
+constexpr int64_t kStreamWgs = 512, kTileWgs = 256;
 constexpr int32_t kMinTiles = 8;
 
 mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int32_t block_size, mbe::AttnQ8Plan *pl) {
@@ -168,8 +169,10 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
     return report(MBE_ERR_BAD_SHAPE, "empty page pool or table");
 
   *pl = mbe::AttnQ8Plan{};
-  pl->rows = 32;
-  const int64_t qtiles = (group * o->max_window_len + pl->rows - 1) / pl->rows;
+  const int64_t seq_rows = group * o->max_window_len;
+  pl->rows = seq_rows <= 32 ? 32 : seq_rows <= 128 ? 128 : 256;
+  const int64_t most_wgs = pl->rows == 32 ? kStreamWgs : kTileWgs;
+  const int64_t qtiles = (seq_rows + pl->rows - 1) / pl->rows;
   const int64_t tiles = (max_kv + mbe::kKeyTile - 1) / mbe::kKeyTile;
   // units within the bounds: qtiles of every sequence, but no more than the rows fill
   const int64_t seq_units = std::min<int64_t>(o->batch * qtiles, o->total_q * group / pl->rows + o->batch);
@@ -177,18 +180,19 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
   const int64_t grid = std::max<int64_t>(1, o->batch * qtiles * kv->num_kv_heads);
   pl->qtiles = static_cast<int32_t>(std::max<int64_t>(1, qtiles));
   pl->min_tiles = o->kv_split_tokens > 0 ? o->kv_split_tokens / mbe::kKeyTile : kMinTiles;
-  pl->split = tiles > pl->min_tiles || grid > kMaxGrid;
+  // (the kernels count the tiles of all units in 32 bits, whatever the lengths within the bounds)
+  pl->split = tiles > pl->min_tiles && grid <= kMaxGrid && grid * tiles < (1LL << 31);
+  if (!pl->split && grid > kMaxGrid) return report(MBE_ERR_BAD_SHAPE, "too many sequences, heads and rows for one call");
   if (!pl->split) {
     pl->wgs = static_cast<int32_t>(grid);
     return MBE_OK;
   }
-  const int64_t most = units > kMaxGrid ? kStreamWgs : (units * tiles + pl->min_tiles - 1) / pl->min_tiles;
-  pl->wgs = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(kStreamWgs, most)));
-  if (pl->wgs > 1) {
-    const size_t part_rows = 2 * static_cast<size_t>(pl->wgs) * pl->rows;
-    pl->part_ml_off = align_up(part_rows * kv->head_dim * sizeof(float));
-    pl->bytes = pl->part_ml_off + align_up(part_rows * 2 * sizeof(float));
-  }
+  const int64_t most = units * ((tiles + pl->min_tiles - 1) / pl->min_tiles);
+  pl->wgs = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most_wgs, most)));
+  const size_t part_rows = 2 * static_cast<size_t>(pl->wgs) * pl->rows;
+  pl->part_o_off = align_up(static_cast<size_t>(pl->wgs) * 8 * sizeof(int32_t));
+  pl->part_ml_off = pl->part_o_off + align_up(part_rows * kv->head_dim * sizeof(float));
+  pl->bytes = pl->part_ml_off + align_up(part_rows * 2 * sizeof(float));
   return MBE_OK;
 }
 
@@ -290,7 +294,8 @@ mbe_status mbe_window_attention_q8(const void *q, const mbe_paged_kv_q8 *paged_k
   p.window_lens = window_lens;
   p.out = static_cast<uint16_t *>(out);
   char *ws = static_cast<char *>(o->workspace);
-  p.part_o = pl.bytes ? reinterpret_cast<float *>(ws) : nullptr;
+  p.notes = pl.bytes ? reinterpret_cast<int32_t *>(ws) : nullptr;
+  p.part_o = pl.bytes ? reinterpret_cast<float *>(ws + pl.part_o_off) : nullptr;
   p.part_ml = pl.bytes ? reinterpret_cast<float *>(ws + pl.part_ml_off) : nullptr;
   p.batch = o->batch;
   p.num_q_heads = o->num_q_heads;

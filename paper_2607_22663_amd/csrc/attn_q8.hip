@@ -22,9 +22,8 @@
 // registers of Q.K the operand of P.V without a shuffle, and V's token-minor
 // page rows (16 keys of a dim, 16 bytes) the other operand.
 //
-// The running maximum is raised only when a tile's exceeds it by 2^8: exact for
-// any reference, and the accumulators are rescaled in a few tiles of a
-// sequence instead of all.
+// The softmax's reference exponent is raised only when a tile's sum overflows a
+// limit (softmax_tile), in a few tiles of a sequence instead of all.
 //
 // Work is dealt on the device, from the device lengths.  A unit is (sequence,
 // KV head, tile of packed rows); all units' 64-key tiles in one line are cut
@@ -49,100 +48,175 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 64;                   // keys of a tile: 4 pages
 constexpr float kNegHuge = -1e30f;
-constexpr float kLazy = 8.f;                // exponent headroom before the reference maximum is raised
-
-__device__ inline int64_t wave_sum(int64_t x) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
-  return x;
-}
 
 // ------------------------------------------------------------ work dealing
-struct Seq {
-  int p, w;                 // prefix and window, clamped to the bounds
-  int tiles, qtiles;        // key tiles, row tiles
+// Sum over the lanes up to this one, by DPP: within rows of 16, then across.
+__device__ inline uint32_t scan_lanes(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast:15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+__device__ inline uint32_t lane_value(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
+// A workgroup's piece of a unit: tiles [ta, tb) of tile range [0, tiles) of row
+// tile qt of KV head g of sequence b, whose window starts at row row0 of q.
+struct Piece {
+  int b, g, qt, p, w, row0, ta, tb, tiles;
 };
 
+// The line of all units' tiles, cut into shares.  With fewer tiles than the
+// workgroups would take at min_tiles each, units are padded to whole shares of
+// min_tiles, so that a workgroup never has pieces of two units; otherwise every
+// workgroup takes an equal share, across units.  (The launch bounds the line to
+// 32 bits.)
 template <int ROWS>
-__device__ inline Seq seq_of(const AttnQ8Params &p, int b) {
-  Seq s;
-  s.p = min(max(p.prefix_lens[b], 0), p.max_prefix);
-  s.w = min(max(p.window_lens[b], 0), p.max_window);
-  s.tiles = static_cast<int>((static_cast<int64_t>(s.p) + s.w + kTile - 1) / kTile);
-  s.qtiles = static_cast<int>((static_cast<int64_t>(s.w) * p.group + ROWS - 1) / ROWS);
-  return s;
-}
+struct Deal {
+  const AttnQ8Params &p;
+  uint32_t share, at, end;      // this workgroup's part of the line: [at, end)
+  uint32_t first;               // its begin
+  bool padded;
 
-template <int ROWS>
-__device__ inline int64_t seq_work(const AttnQ8Params &p, int b) {
-  const Seq s = seq_of<ROWS>(p, b);
-  return static_cast<int64_t>(s.tiles) * s.qtiles * p.num_kv_heads;
-}
-
-// All units' tiles.  Every lane of a wave must call.
-template <int ROWS>
-__device__ inline int64_t total_work(const AttnQ8Params &p) {
-  int64_t sum = 0;
-  for (int b = threadIdx.x & 63; b < p.batch; b += 64) sum += seq_work<ROWS>(p, b);
-  return wave_sum(sum);
-}
-
-// First row of q of sequence b.
-__device__ inline int64_t first_row(const AttnQ8Params &p, int b) {
-  int64_t r = 0;
-  for (int j = threadIdx.x & 63; j < b; j += 64) r += min(max(p.window_lens[j], 0), p.max_window);
-  return wave_sum(r);
-}
-
-struct Unit {
-  int b, g, qt;
-  int64_t begin;            // its first tile in the line
-  Seq s;
-};
-
-// The unit that holds tile t of the line (0 <= t < total_work).
-template <int ROWS>
-__device__ inline Unit unit_at(const AttnQ8Params &p, int64_t t) {
-  const int lane = threadIdx.x & 63;
-  int64_t base = 0;
-  Unit u{};
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    const int b = b0 + lane;
-    const int64_t own = b < p.batch ? seq_work<ROWS>(p, b) : 0;
-    int64_t up = own;       // inclusive prefix sum across the lanes
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t v = __shfl_up(up, o);
-      if (lane >= o) up += v;
-    }
-    const uint64_t past = __builtin_amdgcn_ballot_w64(base + up > t);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      const int64_t start = base + __shfl(up - own, at);
-      u.b = b0 + at;
-      u.s = seq_of<ROWS>(p, u.b);
-      const int64_t rel = t - start;
-      const int unit = static_cast<int>(rel / u.s.tiles);
-      u.g = unit / u.s.qtiles;
-      u.qt = unit - u.g * u.s.qtiles;
-      u.begin = start + static_cast<int64_t>(unit) * u.s.tiles;
-      return u;
-    }
-    base += __shfl(up, 63);
+  __device__ uint32_t whole(uint32_t tiles) const {
+    return padded ? (tiles + share - 1) / share * share : tiles;
   }
-  return u;
+  __device__ void sequence(int b, int &pl, int &wl, uint32_t &tiles, uint32_t &units) const {
+    pl = wl = 0;
+    if (b < p.batch) {
+      pl = min(max(p.prefix_lens[b], 0), p.max_prefix);
+      wl = min(max(p.window_lens[b], 0), p.max_window);
+    }
+    tiles = (static_cast<uint32_t>(pl) + wl + kTile - 1) / kTile;
+    units = (static_cast<uint32_t>(wl) * p.group + ROWS - 1) / ROWS * p.num_kv_heads;
+  }
+
+  // Its first piece; false: it has none.
+  __device__ bool start(Piece &u) {
+    const int lane = threadIdx.x & 63;
+    if (!p.split) {        // a whole unit each
+      const int rest = static_cast<int>(blockIdx.x) / p.qtiles;
+      u.qt = static_cast<int>(blockIdx.x) - rest * p.qtiles;
+      u.b = rest / p.num_kv_heads;
+      u.g = rest - u.b * p.num_kv_heads;
+      uint32_t rows = 0, tiles = 0, units = 0;
+      for (int b0 = 0; b0 <= u.b; b0 += 64) {
+        int pl, wl;
+        sequence(b0 + lane, pl, wl, tiles, units);
+        const uint32_t up = scan_lanes(wl);
+        if (u.b < b0 + 64) {
+          const int l = u.b - b0;
+          u.p = lane_value(pl, l);
+          u.w = lane_value(wl, l);
+          u.tiles = lane_value(tiles, l);
+          u.row0 = rows + lane_value(up, l) - u.w;
+          units = lane_value(units, l);
+        }
+        rows += lane_value(up, 63);
+      }
+      u.ta = 0;
+      u.tb = u.tiles;
+      at = end = 0;
+      return u.qt * p.num_kv_heads < static_cast<int>(units);
+    }
+    uint32_t tight = 0, loose = 0;
+    padded = true;
+    share = p.min_tiles;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      int pl, wl;
+      uint32_t tiles, units;
+      sequence(b0 + lane, pl, wl, tiles, units);
+      tight += lane_value(scan_lanes(tiles * units), 63);
+      loose += lane_value(scan_lanes(whole(tiles) / share * units), 63);     // in shares
+    }
+    padded = loose <= static_cast<uint32_t>(p.wgs);
+    if (!padded) share = max(share, (tight + p.wgs - 1) / p.wgs);
+    const uint32_t total = padded ? loose * share : tight;
+    first = at = share * blockIdx.x;
+    end = min(at + share, total);
+    if (blockIdx.x > (total - 1) / share || total == 0) return false;
+    piece(u);
+    return true;
+  }
+
+  // The piece at `at`.
+  __device__ void piece(Piece &u) {
+    const int lane = threadIdx.x & 63;
+    uint32_t base = 0, rows = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      int pl, wl;
+      uint32_t tiles, units;
+      sequence(b0 + lane, pl, wl, tiles, units);
+      const uint32_t own = whole(tiles) * units, up = scan_lanes(own), wup = scan_lanes(wl);
+      const uint64_t past = __builtin_amdgcn_ballot_w64(base + up > at);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        u.b = b0 + l;
+        u.p = lane_value(pl, l);
+        u.w = lane_value(wl, l);
+        u.tiles = lane_value(tiles, l);
+        u.row0 = rows + lane_value(wup, l) - u.w;
+        const uint32_t rel = at - (base + lane_value(up, l) - lane_value(own, l));
+        const uint32_t length = whole(u.tiles), unit = rel / length, qtiles = lane_value(units, l) / p.num_kv_heads;
+        u.g = unit / qtiles;
+        u.qt = unit - u.g * qtiles;
+        u.ta = rel - unit * length;
+        u.tb = min(static_cast<uint32_t>(u.tiles), u.ta + (end - at));
+        return;
+      }
+      base += lane_value(up, 63);
+      rows += lane_value(wup, 63);
+    }
+  }
+
+  // The next piece of its share; false: it has no more.
+  __device__ bool next(Piece &u) {
+    if (!p.split || padded) return false;
+    at += u.tb - u.ta;
+    if (at >= end) return false;
+    piece(u);
+    return true;
+  }
+
+  // Slot of the partial result of the piece at hand: a share has at most two, its
+  // first piece and its last.
+  __device__ int64_t slot() const { return 2 * static_cast<int64_t>(blockIdx.x) + (at == first ? 0 : 1); }
+};
+
+// What the join kernel is told by the workgroup whose share begins at a unit's
+// first border: the unit's parts lie in slots slot, 2 wg, 2 wg + 2, ...
+struct JoinNote {
+  int32_t parts;            // 0: nothing to join here
+  int32_t b, g, qt, w, row0, slot, unused;
+};
+
+template <int ROWS>
+__device__ inline void leave_note(const AttnQ8Params &p, const Deal<ROWS> &d, const Piece &u, bool any) {
+  if (!p.split || threadIdx.x != 0) return;
+  JoinNote n{};
+  const uint32_t wg = blockIdx.x;
+  if (any && u.ta > 0 && static_cast<uint32_t>(u.ta) <= d.share) {
+    // shares after this one that the unit reaches into
+    const uint32_t left = static_cast<uint32_t>(u.tiles - u.ta);
+    n.parts = 1 + static_cast<int32_t>((left + d.share - 1) / d.share);
+    n.b = u.b;
+    n.g = u.g;
+    n.qt = u.qt;
+    n.w = u.w;
+    n.row0 = u.row0;
+    n.slot = static_cast<int32_t>(2 * (wg - 1) + (static_cast<uint32_t>(u.ta) == d.share ? 0 : 1));
+  }
+  *reinterpret_cast<JoinNote *>(p.notes + 8 * static_cast<int64_t>(wg)) = n;
 }
 
-__device__ inline int64_t share_of(const AttnQ8Params &p, int64_t total) {
-  return max(static_cast<int64_t>(p.min_tiles), (total + p.wgs - 1) / p.wgs);
-}
-
-// Position i of packed row r within the window, and its q row / head.
-__device__ inline bool row_wanted(const AttnQ8Params &p, const Unit &u, int64_t row0, int r) {
-  if (r >= u.s.w * p.group) return false;
+// Whether packed row r of the sequence's KV head is one that the call computes.
+__device__ inline bool row_wanted(const AttnQ8Params &p, int b, int w, int row0, int r) {
+  if (r >= w * p.group) return false;
   const int i = r / p.group;
-  if (row0 + i >= p.total_q) return false;
-  return !p.block_flags || p.block_flags[static_cast<int64_t>(u.b) * p.flag_stride + i / p.block_size] != 0;
+  if (static_cast<int64_t>(row0) + i >= p.total_q) return false;
+  return !p.block_flags || p.block_flags[static_cast<int64_t>(b) * p.flag_stride + i / p.block_size] != 0;
 }
 
 // ------------------------------------------------------------- the pieces
@@ -233,24 +307,105 @@ __device__ inline float load_q(const uint16_t *src, i32x8 *hi, i32x8 *lo) {
   return __uint_as_float(static_cast<uint32_t>(127 - 7 + e) << 23);
 }
 
-__device__ inline int page_of(const AttnQ8Params &p, int b, int64_t slot) {
+// Entry of the page table, as it is: where it is looked at right after the load,
+// the wave waits for every load in flight, so its clamping is left to its use.
+__device__ inline int page_entry(const AttnQ8Params &p, int b, int64_t slot) {
   const int64_t s = min(slot, static_cast<int64_t>(p.max_pages) - 1);
-  return min(max(p.page_table[static_cast<int64_t>(b) * p.max_pages + s], 0), p.num_pages - 1);
+  return p.page_table[static_cast<int64_t>(b) * p.max_pages + s];
+}
+__device__ inline int clamp_page(const AttnQ8Params &p, int entry) { return min(max(entry, 0), p.num_pages - 1); }
+
+// A 32-key block's softmax: s (scores before scaling, -inf where masked) of the
+// lane's 16 keys of one page to packed probabilities times V's scale, relative to
+// the reference exponent m; l and acc follow a raised m.
+//
+// Optimistic: the probabilities are computed against the old reference, and only
+// where a lane's sum exceeds 2^16 (or is no number) does the wave take the
+// block's maximum, raise the reference and compute them again.  Any reference is
+// exact, so the result is off by no more than fp32's rounding, and a block costs
+// no maximum (of 16 values and across lanes).
+constexpr float kSumLimit = 65536.f;
+
+// Raises m to the block's maximum; the sum and the accumulators follow.
+template <int NB>
+__device__ inline void raise_reference(const f32x16 &s, float c, float &m, float &l, f32x16 *acc) {
+  float mt = s[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
+  mt = across_halves_max(fmaxf(kNegHuge, mt * c));
+  const float mn = fmaxf(m, mt);
+  const float a = __builtin_amdgcn_exp2f(m - mn);
+  m = mn;
+  l *= a;
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[j][i] *= a;
+}
+
+template <int NB>
+__device__ inline void softmax_block(const f32x16 &s, float c, float lv, float iv, float &m, float &l, f32x16 *acc, bf16x8 *pb) {
+  float sum;
+  auto exps = [&]() {
+    const float off = lv - m;
+    uint32_t pk[8];
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float a = __builtin_amdgcn_exp2f(fmaf(s[i], c, off)), b = __builtin_amdgcn_exp2f(fmaf(s[i + 1], c, off));
+      t += a;
+      t += b;
+      pk[i / 2] = pack2(a, b);
+    }
+    sum = t * iv;
+    pb[0] = __builtin_bit_cast(bf16x8, (uint4{pk[0], pk[1], pk[2], pk[3]}));
+    pb[1] = __builtin_bit_cast(bf16x8, (uint4{pk[4], pk[5], pk[6], pk[7]}));
+  };
+  exps();
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
+    raise_reference<NB>(s, c, m, l, acc);
+    exps();
+  }
+  l += sum;
+}
+
+// Per page: factor of the scores apart from the row's, logarithm and reciprocal
+// of V's scale.  (Covered pages have positive finite scales; others hold anything.)
+__device__ inline float k_factor(float ks, float cq) { return fmaxf(ks * cq, 1.17549435e-38f); }
+__device__ inline float v_factor(float vs) { return fminf(fmaxf(vs, 0x1p-100f), 0x1p100f); }
+
+// Bytes of a 16-byte row of V, 16 keys, from the `held`th key on to zero: slots
+// behind the last token may hold NaN codes, and 0 x NaN is NaN.
+__device__ inline void zero_behind(uint4 &v, int held) {
+  uint32_t *d = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int nb = min(max(held - 4 * w, 0), 4);
+    d[w] = nb == 4 ? d[w] : d[w] & ((1u << (8 * nb)) - 1u);
+  }
+}
+
+__device__ inline i32x8 operand(uint4 a, uint4 b) {
+  i32x8 k;
+  k[0] = a.x;
+  k[1] = a.y;
+  k[2] = a.z;
+  k[3] = a.w;
+  k[4] = b.x;
+  k[5] = b.y;
+  k[6] = b.z;
+  k[7] = b.w;
+  return k;
 }
 
 // ------------------------------------------------- streaming kernel
 // Units of 32 rows; the workgroup's four waves take key tiles in turn, each
-// straight from HBM into its registers, and join their results in LDS.
+// straight from HBM into its registers, and join their results in LDS.  A tile's
+// K and V registers are loaded again for the wave's next tile right after their
+// last use, so that 8 to 16 KB a wave, and two workgroups on a CU, are always on
+// their way.
 constexpr int kStreamRows = 32;
 constexpr int kStreamWaves = 4;
-
-template <int D, int FMT>
-struct StreamTile {
-  uint4 k[2][D / 32];       // [32-key block][16-byte chunk of the lane's key]
-  uint4 v[2][D / 32];       // [32-key block][32-dim block]: 16 keys of the lane's dim
-  float ks[2], vs[2];       // scales of the lane's page of each block
-  int pid;                  // page (lane & 3) of the tile
-};
 
 template <int D, int FMT>
 __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(AttnQ8Params p) {
@@ -260,43 +415,64 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
   __shared__ __align__(16) float o_lds[kStreamWaves][kStreamRows][kStride];
   __shared__ float ml_lds[kStreamWaves][kStreamRows][2];
   if (p.gate && *p.gate == 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, h = lane >> 5;
-  const int kslot = 4 * (col >> 3) + (col & 3);       // the lane's key (K operand): slot in its page
-  const int kpage = (col >> 2) & 1;                   // and page of the 32-key block
+  const int kpage = (col >> 2) & 1;                   // the lane's key (K operand): its page of the block,
+  const int k_src = (4 * (col >> 3) + (col & 3)) * D + h * 32;     // and byte in the page
 
-  int64_t t0, t1, share = 0;
-  Unit u{};
-  if (p.split) {
-    const int64_t total = total_work<kStreamRows>(p);
-    share = share_of(p, total);
-    t0 = share * blockIdx.x;
-    t1 = min(t0 + share, total);
-    if (t0 >= t1) return;
-    u = unit_at<kStreamRows>(p, t0);
-  } else {
-    const int qt = static_cast<int>(blockIdx.x) % p.qtiles, rest = static_cast<int>(blockIdx.x) / p.qtiles;
-    u.b = rest / p.num_kv_heads;
-    u.g = rest - u.b * p.num_kv_heads;
-    u.qt = qt;
-    u.s = seq_of<kStreamRows>(p, u.b);
-    u.begin = 0;
-    if (qt >= u.s.qtiles) return;
-    t0 = 0;
-    t1 = u.s.tiles;
-  }
-  int64_t t = t0;
-  while (true) {
-    const int ta = static_cast<int>(t - u.begin);
-    const int tb = static_cast<int>(min(t1 - u.begin, static_cast<int64_t>(u.s.tiles)));
-    const int64_t row0 = first_row(p, u.b);
-    const int n = u.s.p + u.s.w;
+  Deal<kStreamRows> deal{p};
+  Piece u;
+  const bool work = deal.start(u);
+  leave_note(p, deal, u, work);
+  if (!work) return;
+  do {
+    const int ta = u.ta, tb = u.tb;
+    const int64_t row0 = u.row0;
+    const int n = u.p + u.w;
     const int r = u.qt * kStreamRows + col;           // packed row of this lane
-    const bool wanted = row_wanted(p, u, row0, r);
+    const bool wanted = row_wanted(p, u.b, u.w, u.row0, r);
     const bool any = __builtin_amdgcn_ballot_w64(wanted) != 0;      // the same in every wave
     if (any) {
       const int wi = r / p.group;
-      const int seen = !wanted ? 0 : (p.causal ? min(n, u.s.p + (wi / p.block_size + 1) * p.block_size) : n);
+      const int seen = !wanted ? 0 : (p.causal ? min(n, u.p + (wi / p.block_size + 1) * p.block_size) : n);
+      // Page table entries of this wave's tiles: lane j of ids holds page j & 3 of
+      // its tile 16 c + (j >> 2), ahead[0] those of the 16 tiles after, ahead[1] of
+      // the next 16.  The pages' scales are gathered likewise, 16 tiles ahead.
+      auto entries = [&](int i) {
+        return page_entry(p, u.b, (static_cast<int64_t>(ta) + wave + static_cast<int64_t>(kStreamWaves) * (i + (lane >> 2))) * 4 + (lane & 3));
+      };
+      int ids = entries(0), ahead[2] = {entries(16), entries(32)};
+      auto head_of = [&](int entry) { return static_cast<int64_t>(clamp_page(p, entry)) * p.num_kv_heads + u.g; };
+      uint4 kx[2][NB], vx[2][NB];         // tile: [32-key block][chunk of the lane's key], [block][32-dim block]
+      auto page_head = [&](int i, int j) { return head_of(__builtin_amdgcn_readlane(ids, (i & 15) * 4 + j)); };
+      auto load_k = [&](int i, int blk) {
+        const int64_t a = page_head(i, 2 * blk), b = page_head(i, 2 * blk + 1);
+        const uint8_t *at = p.k_pages + (kpage ? b : a) * (kPageSize * D) + k_src;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) kx[blk][j] = *reinterpret_cast<const uint4 *>(at + (j >> 1) * 64 + (j & 1) * 16);
+      };
+      auto load_v = [&](int i, int blk) {
+        const int64_t a = page_head(i, 2 * blk), b = page_head(i, 2 * blk + 1);
+        const uint8_t *at = p.v_pages + (h ? b : a) * (kPageSize * D) + col * kPageSize;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) vx[blk][j] = *reinterpret_cast<const uint4 *>(at + j * 32 * kPageSize);
+      };
+      const int mine = (tb - ta - wave + kStreamWaves - 1) / kStreamWaves;       // tiles of this wave
+#pragma unroll
+      for (int blk = 0; blk < 2; ++blk) {
+        load_k(0, blk);
+        load_v(0, blk);
+      }
+      float ks = p.k_scales[head_of(ids)], vs = p.v_scales[head_of(ids)];
+      float ks_next = p.k_scales[head_of(ahead[0])], vs_next = p.v_scales[head_of(ahead[0])];
+      // factor of the scores, V's scale of the lane's page of block blk of the wave's tile i
+      auto scale_of = [&](float x, int i, int blk) {
+        const int at = (i & 15) * 4 + 2 * blk;
+        const float a = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at));
+        const float b = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at + 1));
+        return h ? b : a;
+      };
       i32x8 qh[NS], ql[NS];
       const float qs = load_q<D>(wanted ? p.q + ((row0 + wi) * p.num_q_heads + u.g * p.group + r % p.group) * D : nullptr, qh, ql);
       const float cq = qs * p.scale_log2;
@@ -306,127 +482,49 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
       for (int i = 0; i < NB; ++i) acc[i] = f32x16{};
       float m = kNegHuge, l = 0.f;
 
-      auto pages_of_tile = [&](int tile) { return page_of(p, u.b, static_cast<int64_t>(tile) * 4 + (lane & 3)); };
-      auto load_k = [&](StreamTile<D, FMT> &x) {
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-          const int a = __builtin_amdgcn_readlane(x.pid, 2 * blk), b = __builtin_amdgcn_readlane(x.pid, 2 * blk + 1);
-          const int64_t ph = static_cast<int64_t>(kpage ? b : a) * p.num_kv_heads + u.g;
-          const uint8_t *at = p.k_pages + (ph * kPageSize + kslot) * D + h * 32;
-#pragma unroll
-          for (int j = 0; j < NB; ++j) x.k[blk][j] = *reinterpret_cast<const uint4 *>(at + (j >> 1) * 64 + (j & 1) * 16);
+      for (int i = 0; i < mine; ++i) {
+        const int tile = ta + wave + kStreamWaves * i;
+        // the next tile's entries (behind the last tile: that tile once more, from the cache)
+        const int nx = min(i + 1, mine - 1);
+        if ((i & 15) == 0 && i > 0) {
+          ks = ks_next;
+          vs = vs_next;
+          ks_next = p.k_scales[head_of(ahead[0])];
+          vs_next = p.v_scales[head_of(ahead[0])];
         }
-      };
-      auto load_v = [&](StreamTile<D, FMT> &x) {
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-          const int a = __builtin_amdgcn_readlane(x.pid, 2 * blk), b = __builtin_amdgcn_readlane(x.pid, 2 * blk + 1);
-          const int64_t ph = static_cast<int64_t>(h ? b : a) * p.num_kv_heads + u.g;
-          const uint8_t *at = p.v_pages + (ph * D + col) * kPageSize;
-#pragma unroll
-          for (int j = 0; j < NB; ++j) x.v[blk][j] = *reinterpret_cast<const uint4 *>(at + j * 32 * kPageSize);
-          x.ks[blk] = p.k_scales[ph];
-          x.vs[blk] = p.v_scales[ph];
+        if ((nx & 15) == 0 && nx > i) {
+          ids = ahead[0];
+          ahead[0] = ahead[1];
+          ahead[1] = entries(nx + 32);
         }
-      };
-
-      for (int tile = ta + wave; tile < tb; tile += kStreamWaves) {
-        StreamTile<D, FMT> x;
-        x.pid = pages_of_tile(tile);
-        load_k(x);
-        load_v(x);
-        f32x16 s[2];
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
-          s[blk] = f32x16{};
+          f32x16 s = f32x16{};
 #pragma unroll
           for (int st = 0; st < NS; ++st) {
-            i32x8 k;
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const uint4 c = x.k[blk][2 * st + w];
-              k[4 * w] = c.x;
-              k[4 * w + 1] = c.y;
-              k[4 * w + 2] = c.z;
-              k[4 * w + 3] = c.w;
-            }
-            s[blk] = mfma_qk<FMT>(k, qh[st], s[blk]);
-            s[blk] = mfma_qk<FMT>(k, ql[st], s[blk]);
+            const i32x8 k = operand(kx[blk][2 * st], kx[blk][2 * st + 1]);
+            s = mfma_qk<FMT>(k, qh[st], s);
+            s = mfma_qk<FMT>(k, ql[st], s);
           }
-        }
-        const int key0 = tile * kTile + 16 * h;      // the lane's first key (block 0)
-        // (covered pages have positive finite scales; the others hold anything)
-        float c[2], lv[2], iv[2];
+          const float c = k_factor(scale_of(ks, i, blk), cq), v = v_factor(scale_of(vs, i, blk));
+          load_k(nx, blk);
+          if (tile * kTile + kTile > u.p) {           // not every row sees every key
+            const int key0 = tile * kTile + 32 * blk + 16 * h;
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-          c[blk] = fmaxf(x.ks[blk] * cq, 1.17549435e-38f);
-          const float vs = fminf(fmaxf(x.vs[blk], 0x1p-100f), 0x1p100f);
-          lv[blk] = __builtin_amdgcn_logf(vs);
-          iv[blk] = __builtin_amdgcn_rcpf(vs);
-        }
-        const bool whole = tile * kTile + kTile <= u.s.p;      // every row sees every key
-        if (!whole) {
+            for (int j = 0; j < 16; ++j) s[j] = j < seen - key0 ? s[j] : -__builtin_inff();
 #pragma unroll
-          for (int blk = 0; blk < 2; ++blk) {
-            const int left = seen - (key0 + 32 * blk);
+            for (int j = 0; j < NB; ++j) zero_behind(vx[blk][j], n - key0);
+          }
+          bf16x8 pb[2];
+          softmax_block<NB>(s, c, __builtin_amdgcn_logf(v), __builtin_amdgcn_rcpf(v), m, l, acc, pb);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[blk][i] = i < left ? s[blk][i] : -__builtin_inff();
-            // slots behind the last token may hold NaN codes: 0 x NaN is NaN
-            const int held = n - (key0 + 32 * blk);
+          for (int j2 = 0; j2 < 2; ++j2)
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-              uint32_t *d = reinterpret_cast<uint32_t *>(&x.v[blk][j]);
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const int nb = min(max(held - 4 * w, 0), 4);
-                d[w] = nb == 4 ? d[w] : d[w] & ((1u << (8 * nb)) - 1u);
-              }
+              const uint4 d = vx[blk][j];
+              acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(j2 ? widen8<FMT>(d.z, d.w) : widen8<FMT>(d.x, d.y), pb[j2], acc[j], 0, 0, 0);
             }
-          }
-        }
-        float mt = kNegHuge;
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-          float mb = s[blk][0];
-#pragma unroll
-          for (int i = 1; i < 16; ++i) mb = fmaxf(mb, s[blk][i]);
-          mt = fmaxf(mt, mb * c[blk]);
-        }
-        mt = across_halves_max(mt);
-        if (__builtin_amdgcn_ballot_w64(mt > m + kLazy)) {
-          const float mn = fmaxf(m, mt);
-          const float a = __builtin_amdgcn_exp2f(m - mn);
-          m = mn;
-          l *= a;
-#pragma unroll
-          for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[j][i] *= a;
-        }
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-          const float off = lv[blk] - m;
-          float sum = 0.f;
-          uint32_t pk[8];
-#pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const float a = __builtin_amdgcn_exp2f(fmaf(s[blk][i], c[blk], off));
-            const float b = __builtin_amdgcn_exp2f(fmaf(s[blk][i + 1], c[blk], off));
-            sum += a;
-            sum += b;
-            pk[i / 2] = pack2(a, b);
-          }
-          l = fmaf(sum, iv[blk], l);
-#pragma unroll
-          for (int j2 = 0; j2 < 2; ++j2) {
-            const uint4 pw = {pk[4 * j2], pk[4 * j2 + 1], pk[4 * j2 + 2], pk[4 * j2 + 3]};
-            const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-              const uint32_t *d = reinterpret_cast<const uint32_t *>(&x.v[blk][j]);
-              acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FMT>(d[2 * j2], d[2 * j2 + 1]), pb, acc[j], 0, 0, 0);
-            }
-          }
+          load_v(nx, blk);
         }
       }
       l = across_halves_add(l);
@@ -454,7 +552,7 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
         ll += wt[w] * ml_lds[w][jr][1];
       }
       const int jrow = u.qt * kStreamRows + jr;
-      const bool cut = ta > 0 || tb < u.s.tiles;
+      const bool cut = ta > 0 || tb < u.tiles;
       const float inv = cut ? 1.f : 1.f / ll;
       f32x4 o[D / 32];
 #pragma unroll
@@ -470,7 +568,7 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
         for (int i = 0; i < 4; ++i) o[q][i] *= inv;
       }
       if (cut) {
-        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (t == t0 ? 0 : 1);
+        const int64_t slot = deal.slot();
         float *dst = p.part_o + (slot * kStreamRows + jr) * D + part * (D / 8);
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) *reinterpret_cast<f32x4 *>(dst + 4 * q) = o[q];
@@ -478,7 +576,7 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
           p.part_ml[(slot * kStreamRows + jr) * 2] = mm;
           p.part_ml[(slot * kStreamRows + jr) * 2 + 1] = ll;
         }
-      } else if (row_wanted(p, u, row0, jrow)) {
+      } else if (row_wanted(p, u.b, u.w, u.row0, jrow)) {
         uint16_t *dst = p.out + ((row0 + jrow / p.group) * p.num_q_heads + u.g * p.group + jrow % p.group) * D + part * (D / 8);
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
@@ -488,63 +586,441 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
       }
       __syncthreads();
     }
-    t = u.begin + tb;
-    if (t >= t1) return;
-    u = unit_at<kStreamRows>(p, t);
-  }
+  } while (deal.next(u));
+}
+
+// ------------------------------------------------------- tile kernel
+// Units of 32 * RB rows, RB = 4 or 8: a workgroup of eight waves stages every
+// key tile once in LDS for all its rows.  RB = 8: each wave has 32 rows and sees
+// every tile.  RB = 4: the waves form two groups that take every other tile and
+// join at the end.
+//
+// K goes into LDS as it is (half the bytes bf16 would take), V as bf16, converted
+// once per workgroup on the way: two planes of 8 keys by dim, 16 bytes each, as
+// P.V's operand reads them.  Rows of K lie in the order of the operand's rows,
+// their 16-byte chunks XOR-swizzled so that any eight rows' equal chunks fall on
+// different banks.
+//
+// A wave works on three 32-key blocks at once: while the vector unit turns the
+// scores of block b into probabilities, the matrix unit multiplies the scores of
+// b + 1 and adds P.V of b - 1, all independent.  So iteration t reads K of tiles
+// t and t + 1 and V of t - 1 and t, from three LDS buffers each; it writes K of
+// t + 2 and V of t + 1 from registers and loads K of t + 3 and V of t + 2: one
+// barrier a tile, and a whole tile's time for a load.
+constexpr int kTileThreads = 512;
+
+template <int D, int FMT, int RB>
+__global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Params p) {
+  constexpr int kRows = 32 * RB;
+  constexpr int KS = 8 / RB;              // tiles of an iteration
+  constexpr int NB = D / 32, NS = D / 64;
+  constexpr int kChunks = D / 16;         // 16-byte chunks of a K row
+  constexpr int kItems = 4 * D;           // 16-byte chunks of a tile, of K and of V
+  constexpr bool kHalf = KS * kItems < kTileThreads;     // only the first waves stage
+  constexpr int NI = kHalf ? 1 : KS * kItems / kTileThreads;
+  constexpr int kK = kTile * D, kV = kTile * D * 2;      // bytes of a tile in LDS
+  constexpr int kBuf = KS * (kK + kV);
+  constexpr int kJoin = KS > 1 ? RB * 32 * (D + 4) * 4 : 0;
+  __shared__ __align__(16) uint8_t lds[3 * kBuf > kJoin ? 3 * kBuf : kJoin];
+  __shared__ __align__(16) float sc[3][4 * KS][4];       // per page: K scale, log2 and reciprocal of V's
+  __shared__ float ml[RB][32][2];
+  if (p.gate && *p.gate == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rb = wave % RB, kg = wave / RB;
+  const int col = lane & 31, h = lane >> 5;
+
+  Deal<kRows> deal{p};
+  Piece u;
+  const bool work = deal.start(u);
+  leave_note(p, deal, u, work);
+  if (!work) return;
+  // staging: this thread's 16 bytes of page spage of tile kt0 (+ i) of an
+  // iteration: of K a slot's chunk, of V a dim
+  const int kt0 = __builtin_amdgcn_readfirstlane(tid / kItems);
+  const int spage = __builtin_amdgcn_readfirstlane((tid % kItems) / D), vdim = tid % D;
+  const int kslot = vdim / kChunks, kchunk = vdim % kChunks;
+  const int krow = 32 * (spage >> 1) + 8 * (kslot >> 2) + 4 * (spage & 1) + (kslot & 3);
+  const int k_dst = krow * D + ((kchunk ^ (D == 128 ? krow & 7 : (krow >> 1) & 3)) * 16);
+  const int v_dst = (spage * 2 * D + vdim) * 16;
+  const bool stages = !kHalf || wave < kItems / 64;
+  // operand reads: 16-byte chunks of the lane's K row (block 0), of its V rows
+  int k_at[2 * NS];
+#pragma unroll
+  for (int i = 0; i < 2 * NS; ++i)
+    k_at[i] = kg * kK + col * D + (((4 * (i >> 1) + 2 * h + (i & 1)) ^ (D == 128 ? col & 7 : (col >> 1) & 3)) * 16);
+  const int v_at = KS * kK + kg * kV + (h * 2 * D + col) * 16;
+
+  do {
+    const int ta = u.ta, tb = u.tb;
+    const int64_t row0 = u.row0;
+    const int n = u.p + u.w;
+    const int r = u.qt * kRows + rb * 32 + col;
+    const bool wanted = row_wanted(p, u.b, u.w, u.row0, r);
+    const bool mine = __builtin_amdgcn_ballot_w64(wanted) != 0;
+    if (!p.block_flags || __syncthreads_or(mine)) {
+      const int wi = r / p.group;
+      const int seen = !wanted ? 0 : (p.causal ? min(n, u.p + (wi / p.block_size + 1) * p.block_size) : n);
+      const int64_t q_at = ((row0 + wi) * p.num_q_heads + u.g * p.group + r % p.group) * D;
+
+      uint4 kr[NI], vr[NI];
+      float ksr[NI], vsr[NI];
+      const int iters = (tb - ta + KS - 1) / KS;
+      // Page table entries of this wave's page: lane j of ids[i] holds that of
+      // iteration 64 c + j (tile kt0 + i), ahead[i] those of the 64 after.
+      int ids[NI], ahead[NI];
+      auto entries = [&](int it0, int i) {
+        return page_entry(p, u.b, (static_cast<int64_t>(ta) + static_cast<int64_t>(KS) * (it0 + lane) + kt0 + i) * 4 + spage);
+      };
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        ids[i] = entries(0, i);
+        ahead[i] = entries(64, i);
+      }
+      // (page, head) row of the pools for iteration it, asked for in order
+      auto page_head = [&](int it, int i) {
+        return static_cast<int64_t>(clamp_page(p, __builtin_amdgcn_readlane(ids[i], it & 63))) * p.num_kv_heads + u.g;
+      };
+      auto load_k = [&](const int64_t *ph) {
+        if (!stages) return;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          kr[i] = *reinterpret_cast<const uint4 *>(p.k_pages + ph[i] * (kPageSize * D) + vdim * 16);
+          ksr[i] = p.k_scales[ph[i]];
+          vsr[i] = p.v_scales[ph[i]];
+        }
+      };
+      auto load_v = [&](const int64_t *ph) {
+        if (!stages) return;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+          vr[i] = *reinterpret_cast<const uint4 *>(p.v_pages + ph[i] * (kPageSize * D) + vdim * 16);
+      };
+      auto stage_k = [&](uint8_t *buf, int sbuf) {
+        if (!stages) return;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          *reinterpret_cast<uint4 *>(buf + (kt0 + i) * kK + k_dst) = kr[i];
+          const float vs = v_factor(vsr[i]);
+          const f32x4 w = {ksr[i], __builtin_amdgcn_logf(vs), __builtin_amdgcn_rcpf(vs), 0.f};
+          if (vdim == 0) *reinterpret_cast<f32x4 *>(sc[sbuf][(kt0 + i) * 4 + spage]) = w;
+        }
+      };
+      auto stage_v = [&](uint8_t *buf, int it) {
+        if (!stages) return;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int key = (ta + KS * it + kt0 + i) * kTile;
+          if (key + kTile > n) zero_behind(vr[i], n - (key + spage * 16));
+          bf16x8 *at = reinterpret_cast<bf16x8 *>(buf + KS * kK + (kt0 + i) * kV + v_dst);
+          at[0] = widen8<FMT>(vr[i].x, vr[i].y);
+          at[D] = widen8<FMT>(vr[i].z, vr[i].w);
+        }
+      };
+
+      // tiles 0 and 1 of K, 0 of V in LDS; tile 2 of K, 1 of V on their way
+      int64_t ph_k[NI], ph_v[NI], ph_0[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        ph_0[i] = page_head(0, i);
+        ph_v[i] = page_head(1, i);
+        ph_k[i] = page_head(2, i);
+      }
+      load_k(ph_0);
+      load_v(ph_0);
+      stage_k(lds, 0);
+      load_k(ph_v);
+      stage_v(lds, 0);
+      load_v(ph_v);
+      stage_k(lds + kBuf, 1);
+      load_k(ph_k);
+
+      i32x8 qh[NS], ql[NS];
+      const float qs = load_q<D>(wanted ? p.q + q_at : nullptr, qh, ql);
+      const float cq = qs * p.scale_log2;
+      f32x16 acc[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) acc[i] = f32x16{};
+      float m = kNegHuge, l = 0.f;
+
+      f32x16 s0, s1;
+      bf16x8 p0[2], p1[2];
+      p1[0] = p1[1] = bf16x8{};
+      auto scores = [&](f32x16 &s, const uint8_t *buf, int blk) {
+        s = f32x16{};
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+          const i32x8 k = operand(*reinterpret_cast<const uint4 *>(buf + k_at[2 * st] + blk * 32 * D),
+                                  *reinterpret_cast<const uint4 *>(buf + k_at[2 * st + 1] + blk * 32 * D));
+          s = mfma_qk<FMT>(k, qh[st], s);
+          s = mfma_qk<FMT>(k, ql[st], s);
+        }
+      };
+      auto add_pv = [&](const bf16x8 *pp, const uint8_t *buf, int blk) {
+        const bf16x8 *va = reinterpret_cast<const bf16x8 *>(buf + v_at) + blk * 4 * D;
+#pragma unroll
+        for (int j2 = 0; j2 < 2; ++j2)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+            acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j2 * D + j * 32], pp[j2], acc[j], 0, 0, 0);
+      };
+      // probabilities of block blk of a tile from its scores; the scores of the
+      // next block and P.V of the one before beside them
+      auto block = [&](f32x16 &s, f32x16 &sn, const uint8_t *kbuf, int kblk_, const bf16x8 *pp, const uint8_t *vbuf, int vblk,
+                       bf16x8 *pc, const float *scale, int key0, int last, bool masked) {
+        if (masked) {
+          const int left = last - (key0 + 16 * h);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = i < left ? s[i] : -__builtin_inff();
+        }
+        // K's operands on their way first, V's between the products with K: all at
+        // once, the eight waves' reads would queue up behind each other
+        const f32x4 w = *reinterpret_cast<const f32x4 *>(scale + 4 * h);
+        uint4 ko[2 * NS];
+        bf16x8 vo[2 * NB];
+#pragma unroll
+        for (int i = 0; i < 2 * NS; ++i) ko[i] = *reinterpret_cast<const uint4 *>(kbuf + k_at[i] + kblk_ * 32 * D);
+        const bf16x8 *va = reinterpret_cast<const bf16x8 *>(vbuf + v_at) + vblk * 4 * D;
+        __builtin_amdgcn_sched_barrier(0);
+        const float c = k_factor(w[0], cq);
+        float off = w[1] - m, sum, e[16], t[2] = {0.f, 0.f};
+        auto value = [&](int i) {
+          e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, off));
+          t[i & 1] += e[i];
+          if (i & 1) {
+            const uint32_t w2 = pack2(e[i - 1], e[i]);
+            uint4 x = __builtin_bit_cast(uint4, pc[i >> 3]);
+            reinterpret_cast<uint32_t *>(&x)[(i >> 1) & 3] = w2;
+            pc[i >> 3] = __builtin_bit_cast(bf16x8, x);
+          }
+        };
+        // then the vector unit's work between the matrix unit's: the first values
+        // while the operands arrive
+        constexpr int kMfma = 2 * NS + 2 * NB, kFirst = 16 - kMfma > 4 ? 4 : 16 - kMfma;
+        int v = 0;
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) value(v++);
+        __builtin_amdgcn_sched_barrier(0);
+        sn = f32x16{};
+#pragma unroll
+        for (int i = 0; i < kMfma; ++i) {
+          if (i < 2 * NS) {
+#pragma unroll
+            for (int j = i * NB / NS; j < (i + 1) * NB / NS; ++j) vo[j] = va[(j / NB) * D + (j % NB) * 32];
+          }
+          if (i < 2 * NS)
+            sn = mfma_qk<FMT>(operand(ko[i & ~1], ko[i | 1]), i & 1 ? ql[i >> 1] : qh[i >> 1], sn);
+          else
+            acc[(i - 2 * NS) % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vo[i - 2 * NS], pp[(i - 2 * NS) / NB], acc[(i - 2 * NS) % NB], 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < (16 - kFirst) * (i + 1) / kMfma - (16 - kFirst) * i / kMfma; ++j) value(v++);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        sum = (t[0] + t[1]) * w[2];
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
+          raise_reference<NB>(s, c, m, l, acc);
+          off = w[1] - m;
+          t[0] = t[1] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) value(i);
+          sum = (t[0] + t[1]) * w[2];
+        }
+        l += sum;
+      };
+
+      __syncthreads();
+      if (mine) scores(s0, lds, 0);
+      // buffers of tiles it, it + 1, it + 2, and of it - 1 (the first P.V adds zeros: any V in place will do)
+      uint8_t *b0 = lds, *b1 = lds + kBuf, *b2 = lds + 2 * kBuf, *prev = lds;
+      int i0 = 0, i1 = 1, i2 = 2;
+      for (int it = 0; it < iters; ++it) {
+        const int tile = ta + KS * it + kg;
+        const int last = tile < tb ? seen : 0;
+        const bool masked = tile >= tb || tile * kTile + kTile > u.p;
+        if (mine) block(s0, s1, b0, 1, p1, prev, 1, p0, sc[i0][kg * 4], tile * kTile, last, masked);
+        stage_v(b1, it + 1);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) ph_v[i] = ph_k[i];
+        load_v(ph_v);
+        if (mine) block(s1, s0, b1, 0, p0, b0, 0, p1, sc[i0][kg * 4 + 2], tile * kTile + 32, last, masked);
+        stage_k(b2, i2);
+        if (((it + 3) & 63) == 0) {
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            ids[i] = ahead[i];
+            ahead[i] = entries(it + 3 + 64, i);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) ph_k[i] = page_head(it + 3, i);
+        __syncthreads();
+        load_k(ph_k);
+        prev = b0;
+        b0 = b1;
+        b1 = b2;
+        b2 = prev;
+        const int i = i0;
+        i0 = i1;
+        i1 = i2;
+        i2 = i;
+      }
+      if (mine) add_pv(p1, prev, 1);
+      l = across_halves_add(l);
+      if constexpr (KS > 1) {
+        float (*o_lds)[32][D + 4] = reinterpret_cast<float (*)[32][D + 4]>(lds);
+        __syncthreads();
+        if (kg == 1) {
+          if (h == 0) {
+            ml[rb][col][0] = m;
+            ml[rb][col][1] = l;
+          }
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+              *reinterpret_cast<f32x4 *>(&o_lds[rb][col][j * 32 + 8 * a + 4 * h]) =
+                  f32x4{acc[j][4 * a], acc[j][4 * a + 1], acc[j][4 * a + 2], acc[j][4 * a + 3]};
+        }
+        __syncthreads();
+        if (kg == 0) {
+          const float m2 = ml[rb][col][0], l2 = ml[rb][col][1];
+          const float mn = fmaxf(m, m2);
+          const float wa = __builtin_amdgcn_exp2f(m - mn), wb = __builtin_amdgcn_exp2f(m2 - mn);
+          m = mn;
+          l = l * wa + l2 * wb;
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+              const f32x4 o = *reinterpret_cast<const f32x4 *>(&o_lds[rb][col][j * 32 + 8 * a + 4 * h]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[j][4 * a + i] = acc[j][4 * a + i] * wa + o[i] * wb;
+            }
+        }
+      }
+      if (kg == 0) {
+        if (ta > 0 || tb < u.tiles) {
+          const int64_t at = deal.slot() * kRows + rb * 32 + col;
+          if (h == 0) {
+            p.part_ml[at * 2] = m;
+            p.part_ml[at * 2 + 1] = l;
+          }
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+              *reinterpret_cast<f32x4 *>(p.part_o + at * D + j * 32 + 8 * a + 4 * h) =
+                  f32x4{acc[j][4 * a], acc[j][4 * a + 1], acc[j][4 * a + 2], acc[j][4 * a + 3]};
+        } else if (wanted) {
+          const float inv = 1.f / l;
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+              *reinterpret_cast<uint2 *>(p.out + q_at + j * 32 + 8 * a + 4 * h) =
+                  uint2{pack2(acc[j][4 * a] * inv, acc[j][4 * a + 1] * inv), pack2(acc[j][4 * a + 2] * inv, acc[j][4 * a + 3] * inv)};
+        }
+      }
+      __syncthreads();
+    }
+  } while (deal.next(u));
 }
 
 // ------------------------------------------------------------- the join
-// Workgroup x looks at the border between shares x and x + 1.  Where it is the
-// first border inside a unit, the workgroup joins that unit's parts; y takes
-// eight rows each.
-template <int D, int ROWS>
+// Workgroup x joins the unit that the note of share x + 1 names, if it names one.
+// A block takes RPB rows of it; a row's dims lie across D / 4 lanes, and its parts
+// are dealt to G groups of lanes, whose results meet in LDS.
+template <int D, int ROWS, int RPB>
 __global__ __launch_bounds__(256) void attn_q8_join_kernel(AttnQ8Params p) {
+  constexpr int kLanes = D / 4, G = 256 / (kLanes * RPB);
+  __shared__ __align__(16) float o_lds[RPB][G][D];
+  __shared__ float ml_lds[RPB][G][2];
   if (p.gate && *p.gate == 0) return;
-  const int64_t total = total_work<ROWS>(p);
-  const int64_t share = share_of(p, total);
-  const int64_t border = share * (static_cast<int64_t>(blockIdx.x) + 1);
-  if (border >= total) return;
-  const Unit u = unit_at<ROWS>(p, border);
-  if (u.begin >= border || border - share > u.begin) return;      // at the unit's start, or not its first border
-  const int64_t row0 = first_row(p, u.b);
-  constexpr int kLanes = D / 4;                     // lanes of a row, 4 dims each
-  const int r_in = static_cast<int>(blockIdx.y) * (256 / kLanes) + static_cast<int>(threadIdx.x) / kLanes;
-  const int d = (static_cast<int>(threadIdx.x) % kLanes) * 4;
-  const int r = u.qt * ROWS + r_in;
-  if (!row_wanted(p, u, row0, r)) return;
-  const int64_t end = u.begin + u.s.tiles;
-  const int64_t w0 = u.begin / share, w1 = (end - 1) / share;
+  const int64_t wg = static_cast<int64_t>(blockIdx.x) + 1;
+  const JoinNote n = *reinterpret_cast<const JoinNote *>(p.notes + 8 * wg);
+  if (n.parts == 0) return;
+  const int tid = threadIdx.x, lane = tid % kLanes, group = tid / kLanes % G, row = tid / (kLanes * G);
+  const int r_in = static_cast<int>(blockIdx.y) * RPB + row, r = n.qt * ROWS + r_in;
+  const bool wanted = row_wanted(p, n.b, n.w, n.row0, r);
+  if (RPB == 1 ? !wanted : !__syncthreads_or(wanted)) return;
   float m = kNegHuge, l = 0.f;
   f32x4 o = {};
-  for (int64_t w = w0; w <= w1; ++w) {
-    // the share that the unit begins in holds it second, unless it begins there too
-    const int64_t slot = 2 * w + (w == w0 && u.begin != w * share ? 1 : 0);
-    const float pm = p.part_ml[(slot * ROWS + r_in) * 2], pl = p.part_ml[(slot * ROWS + r_in) * 2 + 1];
-    const f32x4 v = *reinterpret_cast<const f32x4 *>(p.part_o + (slot * ROWS + r_in) * D + d);
-    const float mn = fmaxf(m, pm);
-    const float a = __builtin_amdgcn_exp2f(m - mn), b = __builtin_amdgcn_exp2f(pm - mn);
-    m = mn;
-    l = l * a + pl * b;
+  constexpr int U = 4;                              // parts in flight
+  for (int i0 = group; i0 < n.parts; i0 += G * U) {
+    float pm[U], pl[U];
+    f32x4 v[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = o[i] * a + v[i] * b;
+    for (int k = 0; k < U; ++k) {
+      const int i = min(i0 + k * G, n.parts - 1);
+      const int64_t at = (i == 0 ? n.slot : 2 * (wg + i - 1)) * ROWS + r_in;
+      pm[k] = p.part_ml[at * 2];
+      pl[k] = p.part_ml[at * 2 + 1];
+      v[k] = *reinterpret_cast<const f32x4 *>(p.part_o + at * D + lane * 4);
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (i0 + k * G >= n.parts) continue;
+      const float mn = fmaxf(m, pm[k]);
+      const float a = __builtin_amdgcn_exp2f(m - mn), b = __builtin_amdgcn_exp2f(pm[k] - mn);
+      m = mn;
+      l = l * a + pl[k] * b;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * a + v[k][j] * b;
+    }
   }
+  if constexpr (G > 1) {
+    *reinterpret_cast<f32x4 *>(&o_lds[row][group][lane * 4]) = o;
+    if (lane == 0) {
+      ml_lds[row][group][0] = m;
+      ml_lds[row][group][1] = l;
+    }
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int k = 1; k < G; ++k) {
+      const float pm = ml_lds[row][k][0], pl = ml_lds[row][k][1];
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(&o_lds[row][k][lane * 4]);
+      const float mn = fmaxf(m, pm);
+      const float a = __builtin_amdgcn_exp2f(m - mn), b = __builtin_amdgcn_exp2f(pm - mn);
+      m = mn;
+      l = l * a + pl * b;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * a + v[j] * b;
+    }
+  }
+  if (!wanted) return;
   const float inv = 1.f / l;
-  uint16_t *dst = p.out + ((row0 + r / p.group) * p.num_q_heads + u.g * p.group + r % p.group) * D + d;
-  const uint2 w = {pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
-  *reinterpret_cast<uint2 *>(dst) = w;
+  uint16_t *dst = p.out + ((static_cast<int64_t>(n.row0) + r / p.group) * p.num_q_heads + n.g * p.group + r % p.group) * D + lane * 4;
+  *reinterpret_cast<uint2 *>(dst) = uint2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+}
+
+// Few rows can have many parts: two rows a block.  Many rows have few parts each.
+template <int D, int ROWS>
+void launch_join(const AttnQ8Params &p, hipStream_t stream) {
+  constexpr int kRows = ROWS <= 32 ? 2 : 256 / (D / 4);
+  hipLaunchKernelGGL((attn_q8_join_kernel<D, ROWS, kRows>), dim3(static_cast<unsigned>(p.wgs - 1), ROWS / kRows), dim3(256),
+                     0, stream, p);
 }
 
 template <int D, int FMT>
 hipError_t launch(const AttnQ8Params &p, const AttnQ8Plan &plan, hipStream_t stream) {
-  hipLaunchKernelGGL((attn_q8_stream_kernel<D, FMT>), dim3(static_cast<unsigned>(plan.wgs)), dim3(kStreamWaves * 64), 0,
-                     stream, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !plan.split || plan.wgs < 2) return e;
-  const int rows = 256 / (D / 4);
-  hipLaunchKernelGGL((attn_q8_join_kernel<D, kStreamRows>), dim3(static_cast<unsigned>(plan.wgs - 1), kStreamRows / rows),
-                     dim3(256), 0, stream, p);
-  return hipGetLastError();
+  const dim3 grid(static_cast<unsigned>(plan.wgs));
+  const bool join = plan.split && plan.wgs > 1;
+  hipError_t e;
+  if (plan.rows == 32) {
+    hipLaunchKernelGGL((attn_q8_stream_kernel<D, FMT>), grid, dim3(kStreamWaves * 64), 0, stream, p);
+    e = hipGetLastError();
+    if (e == hipSuccess && join) launch_join<D, 32>(p, stream);
+  } else if (plan.rows == 128) {
+    hipLaunchKernelGGL((attn_q8_tile_kernel<D, FMT, 4>), grid, dim3(kTileThreads), 0, stream, p);
+    e = hipGetLastError();
+    if (e == hipSuccess && join) launch_join<D, 128>(p, stream);
+  } else {
+    hipLaunchKernelGGL((attn_q8_tile_kernel<D, FMT, 8>), grid, dim3(kTileThreads), 0, stream, p);
+    e = hipGetLastError();
+    if (e == hipSuccess && join) launch_join<D, 256>(p, stream);
+  }
+  return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace

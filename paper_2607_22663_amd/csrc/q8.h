@@ -52,7 +52,8 @@ struct AttnQ8Params {
   const int32_t *page_table;         // [batch][max_pages]
   const int32_t *prefix_lens, *window_lens;
   uint16_t *out;                     // bf16 [total_q][Hq][D]
-  float *part_o;                     // fp32 [2 * wgs][rows][D]    (see attn_q8.hip)
+  int32_t *notes;                    // [wgs][8]                   (split only; see attn_q8.hip)
+  float *part_o;                     // fp32 [2 * wgs][rows][D]
   float *part_ml;                    // fp32 [2 * wgs][rows][2]
   int32_t batch, num_q_heads, num_kv_heads, group, num_pages, max_pages;
   int32_t block_size, total_q, max_prefix, max_window, causal;
@@ -70,7 +71,7 @@ struct AttnQ8Params {
 struct AttnQ8Plan {
   int32_t rows;       // packed query rows of a unit
   int32_t qtiles, wgs, min_tiles, split;
-  size_t part_ml_off, bytes;
+  size_t part_o_off, part_ml_off, bytes;
 };
 hipError_t launch_attn_q8(const AttnQ8Params &p, const AttnQ8Plan &plan, int head_dim, int format, hipStream_t stream);
 

@@ -162,8 +162,10 @@ def test_attention_workspace(lib):
     assert lib.mbe_window_attention_q8_workspace_size(None, ctypes.byref(_opts())) == bad
     assert lib.mbe_window_attention_q8_workspace_size(ctypes.byref(_kv()), None) == bad
     # the largest bounds neither overflow nor ask for more than the shares hold
-    huge = size(batch=1 << 30, max_prefix_len=1 << 29, max_window_len=1 << 20, total_q=2 ** 31 - 1, max_pages_per_seq=1)
-    assert 0 < huge < 1 << 32
+    wide = dict(max_window_len=256, max_pages_per_seq=1)
+    assert 0 < size(batch=1024, max_prefix_len=1 << 20, total_q=1 << 18, **wide) < 1 << 28
+    assert size(batch=1024, max_prefix_len=1 << 29, total_q=1 << 18, **wide) == 0      # (too many tiles to deal out)
+    assert size(batch=1 << 30, max_prefix_len=1 << 29, total_q=2 ** 31 - 1, **wide) == bad
     # the binding's query agrees
     q = torch.empty(64, 16, 128, device="meta")
     k = torch.empty(10, 4, 16, 128, dtype=torch.float8_e4m3fn, device="meta")
