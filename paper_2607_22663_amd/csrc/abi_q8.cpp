@@ -170,7 +170,7 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
 
   *pl = mbe::AttnQ8Plan{};
   const int64_t seq_rows = group * o->max_window_len;
-  pl->rows = seq_rows <= 32 ? 32 : seq_rows <= 128 ? 128 : 256;
+  pl->rows = seq_rows <= 32 ? 32 : seq_rows <= 64 ? 64 : seq_rows <= 128 ? 128 : 256;
   const int64_t most_wgs = pl->rows == 32 ? kStreamWgs : kTileWgs;
   const int64_t qtiles = (seq_rows + pl->rows - 1) / pl->rows;
   const int64_t tiles = (max_kv + mbe::kKeyTile - 1) / mbe::kKeyTile;

@@ -34,6 +34,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "q8.h"
 
 namespace mbe {
@@ -376,13 +378,12 @@ __device__ inline float v_factor(float vs) { return fminf(fmaxf(vs, 0x1p-100f), 
 
 // Bytes of a 16-byte row of V, 16 keys, from the `held`th key on to zero: slots
 // behind the last token may hold NaN codes, and 0 x NaN is NaN.
-__device__ inline void zero_behind(uint4 &v, int held) {
-  uint32_t *d = reinterpret_cast<uint32_t *>(&v);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int nb = min(max(held - 4 * w, 0), 4);
-    d[w] = nb == 4 ? d[w] : d[w] & ((1u << (8 * nb)) - 1u);
-  }
+__device__ inline uint32_t keys_of(uint32_t d, int held) {       // of 4 keys
+  const int nb = min(max(held, 0), 4);
+  return nb == 4 ? d : d & ((1u << (8 * nb)) - 1u);
+}
+__device__ inline uint4 zero_behind(uint4 v, int held) {
+  return uint4{keys_of(v.x, held), keys_of(v.y, held - 4), keys_of(v.z, held - 8), keys_of(v.w, held - 12)};
 }
 
 __device__ inline i32x8 operand(uint4 a, uint4 b) {
@@ -513,7 +514,7 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[j] = j < seen - key0 ? s[j] : -__builtin_inff();
 #pragma unroll
-            for (int j = 0; j < NB; ++j) zero_behind(vx[blk][j], n - key0);
+            for (int j = 0; j < NB; ++j) vx[blk][j] = zero_behind(vx[blk][j], n - key0);
           }
           bf16x8 pb[2];
           softmax_block<NB>(s, c, __builtin_amdgcn_logf(v), __builtin_amdgcn_rcpf(v), m, l, acc, pb);
@@ -589,339 +590,280 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
   } while (deal.next(u));
 }
 
-// ------------------------------------------------------- tile kernel
-// Units of 32 * RB rows, RB = 4 or 8: a workgroup of eight waves stages every
-// key tile once in LDS for all its rows.  RB = 8: each wave has 32 rows and sees
-// every tile.  RB = 4: the waves form two groups that take every other tile and
-// join at the end.
+// ------------------------------------------------------- wide kernel
+// Units of 64 * RG rows, RG = 1, 2 or 4: four waves of 64 rows each, one on a
+// SIMD, RG of them side by side on the rows and the others on further key tiles
+// in turn.  Nothing goes through LDS but the final join of the tiles' groups: each
+// wave loads K and V straight into operand registers, as the streaming kernel
+// does, uses them for both of its 32-row blocks, and waves on the same tile share
+// the loads through the CU's cache.
 //
-// K goes into LDS as it is (half the bytes bf16 would take), V as bf16, converted
-// once per workgroup on the way: two planes of 8 keys by dim, 16 bytes each, as
-// P.V's operand reads them.  Rows of K lie in the order of the operand's rows,
-// their 16-byte chunks XOR-swizzled so that any eight rows' equal chunks fall on
-// different banks.
-//
-// A wave works on three 32-key blocks at once: while the vector unit turns the
-// scores of block b into probabilities, the matrix unit multiplies the scores of
-// b + 1 and adds P.V of b - 1, all independent.  So iteration t reads K of tiles
-// t and t + 1 and V of t - 1 and t, from three LDS buffers each; it writes K of
-// t + 2 and V of t + 1 from registers and loads K of t + 3 and V of t + 2: one
-// barrier a tile, and a whole tile's time for a load.
-constexpr int kTileThreads = 512;
-
-template <int D, int FMT, int RB>
-__global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Params p) {
-  constexpr int kRows = 32 * RB;
-  constexpr int KS = 8 / RB;              // tiles of an iteration
+// A wave works on three (32-key block, row block) pairs at once: while the vector
+// unit turns one's scores into probabilities, the matrix unit multiplies the next
+// one's scores and adds P.V of the one before, all independent, instruction by
+// instruction in turn.
+template <int D, int FMT, int RG>
+__global__ __launch_bounds__(256, 1) void attn_q8_wide_kernel(AttnQ8Params p) {
+  constexpr int kRows = 64 * RG, KG = 4 / RG;
   constexpr int NB = D / 32, NS = D / 64;
-  constexpr int kChunks = D / 16;         // 16-byte chunks of a K row
-  constexpr int kItems = 4 * D;           // 16-byte chunks of a tile, of K and of V
-  constexpr bool kHalf = KS * kItems < kTileThreads;     // only the first waves stage
-  constexpr int NI = kHalf ? 1 : KS * kItems / kTileThreads;
-  constexpr int kK = kTile * D, kV = kTile * D * 2;      // bytes of a tile in LDS
-  constexpr int kBuf = KS * (kK + kV);
-  constexpr int kJoin = KS > 1 ? RB * 32 * (D + 4) * 4 : 0;
-  __shared__ __align__(16) uint8_t lds[3 * kBuf > kJoin ? 3 * kBuf : kJoin];
-  __shared__ __align__(16) float sc[3][4 * KS][4];       // per page: K scale, log2 and reciprocal of V's
-  __shared__ float ml[RB][32][2];
+  __shared__ __align__(16) float o_lds[KG > 1 ? (KG - 1) * RG : 1][KG > 1 ? 64 : 1][D + 4];
+  __shared__ float ml_lds[4][64][2];
   if (p.gate && *p.gate == 0) return;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rb = wave % RB, kg = wave / RB;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rg = wave % RG, kg = wave / RG;
   const int col = lane & 31, h = lane >> 5;
+  const int kpage = (col >> 2) & 1;                   // the lane's key (K operand): its page of the block,
+  const int k_src = (4 * (col >> 3) + (col & 3)) * D + h * 32;     // and byte in the page
 
   Deal<kRows> deal{p};
   Piece u;
   const bool work = deal.start(u);
   leave_note(p, deal, u, work);
   if (!work) return;
-  // staging: this thread's 16 bytes of page spage of tile kt0 (+ i) of an
-  // iteration: of K a slot's chunk, of V a dim
-  const int kt0 = __builtin_amdgcn_readfirstlane(tid / kItems);
-  const int spage = __builtin_amdgcn_readfirstlane((tid % kItems) / D), vdim = tid % D;
-  const int kslot = vdim / kChunks, kchunk = vdim % kChunks;
-  const int krow = 32 * (spage >> 1) + 8 * (kslot >> 2) + 4 * (spage & 1) + (kslot & 3);
-  const int k_dst = krow * D + ((kchunk ^ (D == 128 ? krow & 7 : (krow >> 1) & 3)) * 16);
-  const int v_dst = (spage * 2 * D + vdim) * 16;
-  const bool stages = !kHalf || wave < kItems / 64;
-  // operand reads: 16-byte chunks of the lane's K row (block 0), of its V rows
-  int k_at[2 * NS];
-#pragma unroll
-  for (int i = 0; i < 2 * NS; ++i)
-    k_at[i] = kg * kK + col * D + (((4 * (i >> 1) + 2 * h + (i & 1)) ^ (D == 128 ? col & 7 : (col >> 1) & 3)) * 16);
-  const int v_at = KS * kK + kg * kV + (h * 2 * D + col) * 16;
-
   do {
     const int ta = u.ta, tb = u.tb;
-    const int64_t row0 = u.row0;
     const int n = u.p + u.w;
-    const int r = u.qt * kRows + rb * 32 + col;
-    const bool wanted = row_wanted(p, u.b, u.w, u.row0, r);
-    const bool mine = __builtin_amdgcn_ballot_w64(wanted) != 0;
-    if (!p.block_flags || __syncthreads_or(mine)) {
-      const int wi = r / p.group;
-      const int seen = !wanted ? 0 : (p.causal ? min(n, u.p + (wi / p.block_size + 1) * p.block_size) : n);
-      const int64_t q_at = ((row0 + wi) * p.num_q_heads + u.g * p.group + r % p.group) * D;
-
-      uint4 kr[NI], vr[NI];
-      float ksr[NI], vsr[NI];
-      const int iters = (tb - ta + KS - 1) / KS;
-      // Page table entries of this wave's page: lane j of ids[i] holds that of
-      // iteration 64 c + j (tile kt0 + i), ahead[i] those of the 64 after.
-      int ids[NI], ahead[NI];
-      auto entries = [&](int it0, int i) {
-        return page_entry(p, u.b, (static_cast<int64_t>(ta) + static_cast<int64_t>(KS) * (it0 + lane) + kt0 + i) * 4 + spage);
-      };
+    int seen[2];
+    bool wanted[2];
+    int64_t q_at[2];
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        ids[i] = entries(0, i);
-        ahead[i] = entries(64, i);
+    for (int b = 0; b < 2; ++b) {
+      const int r = u.qt * kRows + rg * 64 + b * 32 + col, wi = r / p.group;
+      wanted[b] = row_wanted(p, u.b, u.w, u.row0, r);
+      seen[b] = !wanted[b] ? 0 : (p.causal ? min(n, u.p + (wi / p.block_size + 1) * p.block_size) : n);
+      q_at[b] = ((static_cast<int64_t>(u.row0) + wi) * p.num_q_heads + u.g * p.group + r % p.group) * D;
+    }
+    const bool busy = __builtin_amdgcn_ballot_w64(wanted[0] || wanted[1]) != 0;
+    // (groups on other keys have the same rows: all or none of them are busy)
+    float m[2] = {kNegHuge, kNegHuge}, l[2] = {0.f, 0.f};
+    f32x16 acc[2][NB];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) acc[b][i] = f32x16{};
+    if (busy) {
+      // page table entries and scales, as in the streaming kernel
+      auto entries = [&](int i) {
+        return page_entry(p, u.b, (static_cast<int64_t>(ta) + kg + static_cast<int64_t>(KG) * (i + (lane >> 2))) * 4 + (lane & 3));
+      };
+      int ids = entries(0), ahead[2] = {entries(16), entries(32)};
+      auto head_of = [&](int entry) { return static_cast<int64_t>(clamp_page(p, entry)) * p.num_kv_heads + u.g; };
+      uint4 kx[2][NB], vx[2][NB];
+      auto page_head = [&](int i, int j) { return head_of(__builtin_amdgcn_readlane(ids, (i & 15) * 4 + j)); };
+      auto load_k = [&](int i, int blk) {
+        const int64_t a = page_head(i, 2 * blk), b = page_head(i, 2 * blk + 1);
+        const uint8_t *at = p.k_pages + (kpage ? b : a) * (kPageSize * D) + k_src;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) kx[blk][j] = *reinterpret_cast<const uint4 *>(at + (j >> 1) * 64 + (j & 1) * 16);
+      };
+      auto load_v = [&](int i, int blk) {
+        const int64_t a = page_head(i, 2 * blk), b = page_head(i, 2 * blk + 1);
+        const uint8_t *at = p.v_pages + (h ? b : a) * (kPageSize * D) + col * kPageSize;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) vx[blk][j] = *reinterpret_cast<const uint4 *>(at + j * 32 * kPageSize);
+      };
+      const int mine = (tb - ta - kg + KG - 1) / KG;       // tiles of this wave
+#pragma unroll
+      for (int blk = 0; blk < 2; ++blk) {
+        load_k(0, blk);
+        load_v(0, blk);
       }
-      // (page, head) row of the pools for iteration it, asked for in order
-      auto page_head = [&](int it, int i) {
-        return static_cast<int64_t>(clamp_page(p, __builtin_amdgcn_readlane(ids[i], it & 63))) * p.num_kv_heads + u.g;
+      float ks = p.k_scales[head_of(ids)], vs = p.v_scales[head_of(ids)];
+      float ks_next = p.k_scales[head_of(ahead[0])], vs_next = p.v_scales[head_of(ahead[0])];
+      auto scale_of = [&](float x, int i, int blk) {
+        const int at = (i & 15) * 4 + 2 * blk;
+        const float a = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at));
+        const float b = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at + 1));
+        return h ? b : a;
       };
-      auto load_k = [&](const int64_t *ph) {
-        if (!stages) return;
+      i32x8 qh[2][NS], ql[2][NS];
+      float cq[2];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          kr[i] = *reinterpret_cast<const uint4 *>(p.k_pages + ph[i] * (kPageSize * D) + vdim * 16);
-          ksr[i] = p.k_scales[ph[i]];
-          vsr[i] = p.v_scales[ph[i]];
-        }
-      };
-      auto load_v = [&](const int64_t *ph) {
-        if (!stages) return;
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-          vr[i] = *reinterpret_cast<const uint4 *>(p.v_pages + ph[i] * (kPageSize * D) + vdim * 16);
-      };
-      auto stage_k = [&](uint8_t *buf, int sbuf) {
-        if (!stages) return;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          *reinterpret_cast<uint4 *>(buf + (kt0 + i) * kK + k_dst) = kr[i];
-          const float vs = v_factor(vsr[i]);
-          const f32x4 w = {ksr[i], __builtin_amdgcn_logf(vs), __builtin_amdgcn_rcpf(vs), 0.f};
-          if (vdim == 0) *reinterpret_cast<f32x4 *>(sc[sbuf][(kt0 + i) * 4 + spage]) = w;
-        }
-      };
-      auto stage_v = [&](uint8_t *buf, int it) {
-        if (!stages) return;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int key = (ta + KS * it + kt0 + i) * kTile;
-          if (key + kTile > n) zero_behind(vr[i], n - (key + spage * 16));
-          bf16x8 *at = reinterpret_cast<bf16x8 *>(buf + KS * kK + (kt0 + i) * kV + v_dst);
-          at[0] = widen8<FMT>(vr[i].x, vr[i].y);
-          at[D] = widen8<FMT>(vr[i].z, vr[i].w);
-        }
-      };
-
-      // tiles 0 and 1 of K, 0 of V in LDS; tile 2 of K, 1 of V on their way
-      int64_t ph_k[NI], ph_v[NI], ph_0[NI];
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        ph_0[i] = page_head(0, i);
-        ph_v[i] = page_head(1, i);
-        ph_k[i] = page_head(2, i);
-      }
-      load_k(ph_0);
-      load_v(ph_0);
-      stage_k(lds, 0);
-      load_k(ph_v);
-      stage_v(lds, 0);
-      load_v(ph_v);
-      stage_k(lds + kBuf, 1);
-      load_k(ph_k);
-
-      i32x8 qh[NS], ql[NS];
-      const float qs = load_q<D>(wanted ? p.q + q_at : nullptr, qh, ql);
-      const float cq = qs * p.scale_log2;
-      f32x16 acc[NB];
-#pragma unroll
-      for (int i = 0; i < NB; ++i) acc[i] = f32x16{};
-      float m = kNegHuge, l = 0.f;
+      for (int b = 0; b < 2; ++b) cq[b] = load_q<D>(wanted[b] ? p.q + q_at[b] : nullptr, qh[b], ql[b]) * p.scale_log2;
 
       f32x16 s0, s1;
-      bf16x8 p0[2], p1[2];
-      p1[0] = p1[1] = bf16x8{};
-      auto scores = [&](f32x16 &s, const uint8_t *buf, int blk) {
-        s = f32x16{};
+      bf16x8 p0[2], p1[2], wv[2][NB];
 #pragma unroll
-        for (int st = 0; st < NS; ++st) {
-          const i32x8 k = operand(*reinterpret_cast<const uint4 *>(buf + k_at[2 * st] + blk * 32 * D),
-                                  *reinterpret_cast<const uint4 *>(buf + k_at[2 * st + 1] + blk * 32 * D));
-          s = mfma_qk<FMT>(k, qh[st], s);
-          s = mfma_qk<FMT>(k, ql[st], s);
-        }
-      };
-      auto add_pv = [&](const bf16x8 *pp, const uint8_t *buf, int blk) {
-        const bf16x8 *va = reinterpret_cast<const bf16x8 *>(buf + v_at) + blk * 4 * D;
+      for (int j = 0; j < 2; ++j) {
+        p1[j] = bf16x8{};
 #pragma unroll
-        for (int j2 = 0; j2 < 2; ++j2)
-#pragma unroll
-          for (int j = 0; j < NB; ++j)
-            acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j2 * D + j * 32], pp[j2], acc[j], 0, 0, 0);
-      };
-      // probabilities of block blk of a tile from its scores; the scores of the
-      // next block and P.V of the one before beside them
-      auto block = [&](f32x16 &s, f32x16 &sn, const uint8_t *kbuf, int kblk_, const bf16x8 *pp, const uint8_t *vbuf, int vblk,
-                       bf16x8 *pc, const float *scale, int key0, int last, bool masked) {
-        if (masked) {
-          const int left = last - (key0 + 16 * h);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = i < left ? s[i] : -__builtin_inff();
-        }
-        // K's operands on their way first, V's between the products with K: all at
-        // once, the eight waves' reads would queue up behind each other
-        const f32x4 w = *reinterpret_cast<const f32x4 *>(scale + 4 * h);
-        uint4 ko[2 * NS];
-        bf16x8 vo[2 * NB];
-#pragma unroll
-        for (int i = 0; i < 2 * NS; ++i) ko[i] = *reinterpret_cast<const uint4 *>(kbuf + k_at[i] + kblk_ * 32 * D);
-        const bf16x8 *va = reinterpret_cast<const bf16x8 *>(vbuf + v_at) + vblk * 4 * D;
-        __builtin_amdgcn_sched_barrier(0);
-        const float c = k_factor(w[0], cq);
-        float off = w[1] - m, sum, e[16], t[2] = {0.f, 0.f};
+        for (int i = 0; i < NB; ++i) wv[j][i] = bf16x8{};
+      }
+      // One step: probabilities of block blk, rows b, from s; into sn the scores of
+      // block kblk, rows kb; P.V of pp with the V operands wv (widened here from
+      // block vblk when `fresh`), rows pb.
+      auto step = [&](auto widens, const uint4 (&fresh_v)[NB], f32x16 &s, int b, f32x16 &sn, const uint4 (&k)[NB], int kb,
+                      const bf16x8 (&pp)[2], int pb, bf16x8 (&pc)[2], float ksc, float lv, float iv) {
+        constexpr bool fresh = decltype(widens)::value;
+        const float c = k_factor(ksc, cq[b]);
+        float off = lv - m[b], t[2] = {0.f, 0.f}, e[16];
         auto value = [&](int i) {
           e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, off));
           t[i & 1] += e[i];
           if (i & 1) {
-            const uint32_t w2 = pack2(e[i - 1], e[i]);
             uint4 x = __builtin_bit_cast(uint4, pc[i >> 3]);
-            reinterpret_cast<uint32_t *>(&x)[(i >> 1) & 3] = w2;
+            reinterpret_cast<uint32_t *>(&x)[(i >> 1) & 3] = pack2(e[i - 1], e[i]);
             pc[i >> 3] = __builtin_bit_cast(bf16x8, x);
           }
         };
-        // then the vector unit's work between the matrix unit's: the first values
-        // while the operands arrive
-        constexpr int kMfma = 2 * NS + 2 * NB, kFirst = 16 - kMfma > 4 ? 4 : 16 - kMfma;
-        int v = 0;
-#pragma unroll
-        for (int i = 0; i < kFirst; ++i) value(v++);
+        constexpr int kQ = 2 * NS, kP = 2 * NB;
         __builtin_amdgcn_sched_barrier(0);
         sn = f32x16{};
 #pragma unroll
-        for (int i = 0; i < kMfma; ++i) {
-          if (i < 2 * NS) {
+        for (int i = 0; i < kQ; ++i) {
+          sn = mfma_qk<FMT>(operand(k[i & ~1], k[i | 1]), i & 1 ? ql[kb][i >> 1] : qh[kb][i >> 1], sn);
 #pragma unroll
-            for (int j = i * NB / NS; j < (i + 1) * NB / NS; ++j) vo[j] = va[(j / NB) * D + (j % NB) * 32];
-          }
-          if (i < 2 * NS)
-            sn = mfma_qk<FMT>(operand(ko[i & ~1], ko[i | 1]), i & 1 ? ql[i >> 1] : qh[i >> 1], sn);
-          else
-            acc[(i - 2 * NS) % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vo[i - 2 * NS], pp[(i - 2 * NS) / NB], acc[(i - 2 * NS) % NB], 0, 0, 0);
-#pragma unroll
-          for (int j = 0; j < (16 - kFirst) * (i + 1) / kMfma - (16 - kFirst) * i / kMfma; ++j) value(v++);
+          for (int j = 8 * i / kQ; j < 8 * (i + 1) / kQ; ++j) value(j);
+          if (fresh && i == kQ - 1) wv[0][0] = widen8<FMT>(fresh_v[0].x, fresh_v[0].y);
           __builtin_amdgcn_sched_barrier(0);
         }
-        sum = (t[0] + t[1]) * w[2];
+#pragma unroll
+        for (int i = 0; i < kP; ++i) {
+          acc[pb][i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[i / NB][i % NB], pp[i / NB], acc[pb][i % NB], 0, 0, 0);
+          if (fresh && i + 1 < kP) {
+            const uint4 d = fresh_v[(i + 1) % NB];
+            wv[(i + 1) / NB][(i + 1) % NB] = (i + 1) / NB ? widen8<FMT>(d.z, d.w) : widen8<FMT>(d.x, d.y);
+          }
+#pragma unroll
+          for (int j = 8 + 8 * i / kP; j < 8 + 8 * (i + 1) / kP; ++j) value(j);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        float sum = (t[0] + t[1]) * iv;
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
-          raise_reference<NB>(s, c, m, l, acc);
-          off = w[1] - m;
+          raise_reference<NB>(s, c, m[b], l[b], acc[b]);
+          off = lv - m[b];
           t[0] = t[1] = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) value(i);
-          sum = (t[0] + t[1]) * w[2];
+          sum = (t[0] + t[1]) * iv;
         }
-        l += sum;
+        l[b] += sum;
+      };
+      auto mask = [&](f32x16 &s, int b, int key) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = j < seen[b] - key ? s[j] : -__builtin_inff();
       };
 
-      __syncthreads();
-      if (mine) scores(s0, lds, 0);
-      // buffers of tiles it, it + 1, it + 2, and of it - 1 (the first P.V adds zeros: any V in place will do)
-      uint8_t *b0 = lds, *b1 = lds + kBuf, *b2 = lds + 2 * kBuf, *prev = lds;
-      int i0 = 0, i1 = 1, i2 = 2;
-      for (int it = 0; it < iters; ++it) {
-        const int tile = ta + KS * it + kg;
-        const int last = tile < tb ? seen : 0;
-        const bool masked = tile >= tb || tile * kTile + kTile > u.p;
-        if (mine) block(s0, s1, b0, 1, p1, prev, 1, p0, sc[i0][kg * 4], tile * kTile, last, masked);
-        stage_v(b1, it + 1);
+      s0 = f32x16{};
 #pragma unroll
-        for (int i = 0; i < NI; ++i) ph_v[i] = ph_k[i];
-        load_v(ph_v);
-        if (mine) block(s1, s0, b1, 0, p0, b0, 0, p1, sc[i0][kg * 4 + 2], tile * kTile + 32, last, masked);
-        stage_k(b2, i2);
-        if (((it + 3) & 63) == 0) {
-#pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            ids[i] = ahead[i];
-            ahead[i] = entries(it + 3 + 64, i);
-          }
+      for (int i = 0; i < 2 * NS; ++i)
+        s0 = mfma_qk<FMT>(operand(kx[0][i & ~1], kx[0][i | 1]), i & 1 ? ql[0][i >> 1] : qh[0][i >> 1], s0);
+      for (int i = 0; i < mine; ++i) {
+        const int tile = ta + kg + KG * i;
+        // the next tile's entries (behind the last tile: that tile once more, from the cache)
+        const int nx = min(i + 1, mine - 1);
+        if ((i & 15) == 0 && i > 0) {
+          ks = ks_next;
+          vs = vs_next;
+          ks_next = p.k_scales[head_of(ahead[0])];
+          vs_next = p.v_scales[head_of(ahead[0])];
         }
+        if ((nx & 15) == 0 && nx > i) {
+          ids = ahead[0];
+          ahead[0] = ahead[1];
+          ahead[1] = entries(nx + 32);
+        }
+        const bool masked = tile * kTile + kTile > u.p;
+        const int key = tile * kTile + 16 * h;
+        float v = v_factor(scale_of(vs, i, 0)), k = scale_of(ks, i, 0);
+        float lv = __builtin_amdgcn_logf(v), iv = __builtin_amdgcn_rcpf(v);
+        if (masked) mask(s0, 0, key);
+        step(std::false_type{}, vx[0], s0, 0, s1, kx[0], 1, p1, 1, p0, k, lv, iv);
+        load_k(nx, 0);
+        if (masked) {
+          mask(s1, 1, key);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) ph_k[i] = page_head(it + 3, i);
-        __syncthreads();
-        load_k(ph_k);
-        prev = b0;
-        b0 = b1;
-        b1 = b2;
-        b2 = prev;
-        const int i = i0;
-        i0 = i1;
-        i1 = i2;
-        i2 = i;
+          for (int j = 0; j < NB; ++j) vx[0][j] = zero_behind(vx[0][j], n - key);
+        }
+        step(std::true_type{}, vx[0], s1, 1, s0, kx[1], 0, p0, 0, p1, k, lv, iv);
+        load_v(nx, 0);
+        v = v_factor(scale_of(vs, i, 1)), k = scale_of(ks, i, 1);
+        lv = __builtin_amdgcn_logf(v), iv = __builtin_amdgcn_rcpf(v);
+        if (masked) mask(s0, 0, key + 32);
+        step(std::false_type{}, vx[1], s0, 0, s1, kx[1], 1, p1, 1, p0, k, lv, iv);
+        load_k(nx, 1);
+        if (masked) {
+          mask(s1, 1, key + 32);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) vx[1][j] = zero_behind(vx[1][j], n - (key + 32));
+        }
+        step(std::true_type{}, vx[1], s1, 1, s0, kx[0], 0, p0, 0, p1, k, lv, iv);
+        load_v(nx, 1);
       }
-      if (mine) add_pv(p1, prev, 1);
-      l = across_halves_add(l);
-      if constexpr (KS > 1) {
-        float (*o_lds)[32][D + 4] = reinterpret_cast<float (*)[32][D + 4]>(lds);
-        __syncthreads();
-        if (kg == 1) {
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i)
+        acc[1][i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[i / NB][i % NB], p1[i / NB], acc[1][i % NB], 0, 0, 0);
+      l[0] = across_halves_add(l[0]);
+      l[1] = across_halves_add(l[1]);
+    }
+    if constexpr (KG > 1) {
+      if (kg > 0 && busy) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
           if (h == 0) {
-            ml[rb][col][0] = m;
-            ml[rb][col][1] = l;
+            ml_lds[wave][b * 32 + col][0] = m[b];
+            ml_lds[wave][b * 32 + col][1] = l[b];
           }
 #pragma unroll
           for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int a = 0; a < 4; ++a)
-              *reinterpret_cast<f32x4 *>(&o_lds[rb][col][j * 32 + 8 * a + 4 * h]) =
-                  f32x4{acc[j][4 * a], acc[j][4 * a + 1], acc[j][4 * a + 2], acc[j][4 * a + 3]};
-        }
-        __syncthreads();
-        if (kg == 0) {
-          const float m2 = ml[rb][col][0], l2 = ml[rb][col][1];
-          const float mn = fmaxf(m, m2);
-          const float wa = __builtin_amdgcn_exp2f(m - mn), wb = __builtin_amdgcn_exp2f(m2 - mn);
-          m = mn;
-          l = l * wa + l2 * wb;
-#pragma unroll
-          for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-              const f32x4 o = *reinterpret_cast<const f32x4 *>(&o_lds[rb][col][j * 32 + 8 * a + 4 * h]);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[j][4 * a + i] = acc[j][4 * a + i] * wa + o[i] * wb;
-            }
+              *reinterpret_cast<f32x4 *>(&o_lds[wave - RG][b * 32 + col][j * 32 + 8 * a + 4 * h]) =
+                  f32x4{acc[b][j][4 * a], acc[b][j][4 * a + 1], acc[b][j][4 * a + 2], acc[b][j][4 * a + 3]};
         }
       }
-      if (kg == 0) {
-        if (ta > 0 || tb < u.tiles) {
-          const int64_t at = deal.slot() * kRows + rb * 32 + col;
+      __syncthreads();
+      if (kg == 0 && busy) {
+#pragma unroll
+        for (int o = 1; o < KG; ++o)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int w = o * RG + rg;
+            const float m2 = ml_lds[w][b * 32 + col][0], l2 = ml_lds[w][b * 32 + col][1];
+            const float mn = fmaxf(m[b], m2);
+            const float wa = __builtin_amdgcn_exp2f(m[b] - mn), wb = __builtin_amdgcn_exp2f(m2 - mn);
+            m[b] = mn;
+            l[b] = l[b] * wa + l2 * wb;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+              for (int a = 0; a < 4; ++a) {
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(&o_lds[w - RG][b * 32 + col][j * 32 + 8 * a + 4 * h]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[b][j][4 * a + i] = acc[b][j][4 * a + i] * wa + x[i] * wb;
+              }
+          }
+      }
+      __syncthreads();
+    }
+    if (kg == 0 && busy) {
+      const bool cut = ta > 0 || tb < u.tiles;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if (cut) {
+          const int64_t at = deal.slot() * kRows + rg * 64 + b * 32 + col;
           if (h == 0) {
-            p.part_ml[at * 2] = m;
-            p.part_ml[at * 2 + 1] = l;
+            p.part_ml[at * 2] = m[b];
+            p.part_ml[at * 2 + 1] = l[b];
           }
 #pragma unroll
           for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int a = 0; a < 4; ++a)
               *reinterpret_cast<f32x4 *>(p.part_o + at * D + j * 32 + 8 * a + 4 * h) =
-                  f32x4{acc[j][4 * a], acc[j][4 * a + 1], acc[j][4 * a + 2], acc[j][4 * a + 3]};
-        } else if (wanted) {
-          const float inv = 1.f / l;
+                  f32x4{acc[b][j][4 * a], acc[b][j][4 * a + 1], acc[b][j][4 * a + 2], acc[b][j][4 * a + 3]};
+        } else if (wanted[b]) {
+          const float inv = 1.f / l[b];
 #pragma unroll
           for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int a = 0; a < 4; ++a)
-              *reinterpret_cast<uint2 *>(p.out + q_at + j * 32 + 8 * a + 4 * h) =
-                  uint2{pack2(acc[j][4 * a] * inv, acc[j][4 * a + 1] * inv), pack2(acc[j][4 * a + 2] * inv, acc[j][4 * a + 3] * inv)};
+              *reinterpret_cast<uint2 *>(p.out + q_at[b] + j * 32 + 8 * a + 4 * h) =
+                  uint2{pack2(acc[b][j][4 * a] * inv, acc[b][j][4 * a + 1] * inv),
+                        pack2(acc[b][j][4 * a + 2] * inv, acc[b][j][4 * a + 3] * inv)};
         }
       }
-      __syncthreads();
     }
   } while (deal.next(u));
 }
@@ -1008,15 +950,19 @@ hipError_t launch(const AttnQ8Params &p, const AttnQ8Plan &plan, hipStream_t str
   const bool join = plan.split && plan.wgs > 1;
   hipError_t e;
   if (plan.rows == 32) {
-    hipLaunchKernelGGL((attn_q8_stream_kernel<D, FMT>), grid, dim3(kStreamWaves * 64), 0, stream, p);
+    hipLaunchKernelGGL((attn_q8_stream_kernel<D, FMT>), grid, dim3(256), 0, stream, p);
     e = hipGetLastError();
     if (e == hipSuccess && join) launch_join<D, 32>(p, stream);
+  } else if (plan.rows == 64) {
+    hipLaunchKernelGGL((attn_q8_wide_kernel<D, FMT, 1>), grid, dim3(256), 0, stream, p);
+    e = hipGetLastError();
+    if (e == hipSuccess && join) launch_join<D, 64>(p, stream);
   } else if (plan.rows == 128) {
-    hipLaunchKernelGGL((attn_q8_tile_kernel<D, FMT, 4>), grid, dim3(kTileThreads), 0, stream, p);
+    hipLaunchKernelGGL((attn_q8_wide_kernel<D, FMT, 2>), grid, dim3(256), 0, stream, p);
     e = hipGetLastError();
     if (e == hipSuccess && join) launch_join<D, 128>(p, stream);
   } else {
-    hipLaunchKernelGGL((attn_q8_tile_kernel<D, FMT, 8>), grid, dim3(kTileThreads), 0, stream, p);
+    hipLaunchKernelGGL((attn_q8_wide_kernel<D, FMT, 4>), grid, dim3(256), 0, stream, p);
     e = hipGetLastError();
     if (e == hipSuccess && join) launch_join<D, 256>(p, stream);
   }
