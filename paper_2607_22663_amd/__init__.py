@@ -710,17 +710,39 @@ def _pool_q8_explain(k_pages, v_pages, k_scales, v_scales, page_table):
     _need(page_table, "page_table", _I32, dev, 2)
 
 
-def _ranges_q8(kv, page_table, start_pos, lens, max_len):
+def _ranges_q8(page_table, start_pos, lens, max_len):
     """Checks the ranges of a write or a read; returns (batch, max_len)."""
-    dev = page_table.device
-    _need(start_pos, "start_pos", _I32, dev, 1)
-    _need(lens, "lens", _I32, dev, 1)
-    batch = start_pos.shape[0]
-    if lens.shape[0] != batch or page_table.shape[0] != batch:
+    index = page_table.get_device()
+    try:
+        (batch,) = shape = start_pos.shape
+        usual = (start_pos.dtype is _I32 and lens.dtype is _I32 and lens.shape == shape
+                 and start_pos.get_device() == index and lens.get_device() == index and start_pos.is_contiguous()
+                 and lens.is_contiguous() and page_table.shape[0] == batch)
+    except (AttributeError, ValueError):
+        usual = False
+    if not usual:
+        dev = page_table.device
+        _need(start_pos, "start_pos", _I32, dev, 1)
+        _need(lens, "lens", _I32, dev, 1)
         raise ValueError("page_table, start_pos and lens disagree on the batch size")
     if max_len is None:
         max_len = int(lens.max().item()) if batch else 0
     return batch, int(max_len)
+
+
+def _token_rows(x, y, names, kv, index, device):
+    """Rows of two bf16 [rows, heads, D] tensors of a pool's tokens."""
+    try:
+        rows, heads, d = shape = x.shape
+        if (x.dtype is _BF16 and y.dtype is _BF16 and y.shape == shape and heads == kv.num_kv_heads and d == kv.head_dim
+                and x.get_device() == index and y.get_device() == index and x.is_contiguous() and y.is_contiguous()):
+            return rows
+    except (AttributeError, ValueError):
+        pass
+    _need(x, names[0], _BF16, device, 3)
+    _need(y, names[1], _BF16, device, 3)
+    raise ValueError(f"{names[0]} and {names[1]} must be [rows, {kv.num_kv_heads}, {kv.head_dim}], got "
+                     f"{tuple(x.shape)} and {tuple(y.shape)}")
 
 
 @_on_device
@@ -739,24 +761,23 @@ def kv_write_q8(k_pages, v_pages, k_scales, v_scales, page_table, start_pos, len
     synchronisation).  block_flags, block_size: as for kv_write."""
     lib = load()
     kv = _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table)
-    dev = k_pages.device
-    batch, max_len = _ranges_q8(kv, page_table, start_pos, lens, max_len)
-    _need(k_new, "k_new", _BF16, dev, 3)
-    _need(v_new, "v_new", _BF16, dev, 3)
-    if k_new.shape != v_new.shape or k_new.shape[1] != kv.num_kv_heads or k_new.shape[2] != kv.head_dim:
-        raise ValueError(f"k_new and v_new must be [total_tokens, {kv.num_kv_heads}, {kv.head_dim}], got "
-                         f"{tuple(k_new.shape)} and {tuple(v_new.shape)}")
+    index = k_pages.get_device()
+    batch, max_len = _ranges_q8(page_table, start_pos, lens, max_len)
+    rows = _token_rows(k_new, v_new, ("k_new", "v_new"), kv, index, k_pages.device)
     if kv_lens is not None:
-        _need(kv_lens, "kv_lens", _I32, dev, 1)
+        _need(kv_lens, "kv_lens", _I32, k_pages.device, 1)
         if kv_lens.shape[0] != batch:
             raise ValueError("kv_lens must have one entry per sequence")
     if block_flags is not None:
         if block_size is None or int(block_size) < 1:
             raise ValueError("block_flags needs block_size >= 1")
-        _flags_gate(block_flags, (batch, -(-max_len // int(block_size))), None, dev)
-    _check("mbe_kv_write_q8", lib.mbe_kv_write_q8(
-        ctypes.byref(kv), _ptr(page_table), page_table.shape[1], _ptr(start_pos), _ptr(lens), _ptr(kv_lens), batch,
-        max_len, k_new.shape[0], _ptr(k_new), _ptr(v_new), _ptr(block_flags), int(block_size or 0), _stream(dev)))
+        _flags_gate(block_flags, (batch, -(-max_len // int(block_size))), None, k_pages.device)
+    status = lib.mbe_kv_write_q8(
+        ctypes.byref(kv), page_table.data_ptr(), page_table.shape[1], start_pos.data_ptr(), lens.data_ptr(),
+        _ptr(kv_lens), batch, max_len, rows, k_new.data_ptr(), v_new.data_ptr(), _ptr(block_flags),
+        int(block_size or 0), torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        _check("mbe_kv_write_q8", status)
 
 
 @_on_device
@@ -768,20 +789,19 @@ def kv_read_q8(k_pages, v_pages, k_scales, v_scales, page_table, start_pos, lens
     synchronisation).  out: optional (k, v) tensors to write to."""
     lib = load()
     kv = _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table)
-    dev = k_pages.device
-    batch, max_len = _ranges_q8(kv, page_table, start_pos, lens, max_len)
+    index = k_pages.get_device()
+    batch, max_len = _ranges_q8(page_table, start_pos, lens, max_len)
     if out is None:
         rows = int(lens.sum().item()) if total is None else int(total)
-        out = tuple(torch.empty(rows, kv.num_kv_heads, kv.head_dim, dtype=_BF16, device=dev) for _ in range(2))
+        out = tuple(torch.empty(rows, kv.num_kv_heads, kv.head_dim, dtype=_BF16, device=k_pages.device)
+                    for _ in range(2))
     k, v = out
-    _need(k, "out[0]", _BF16, dev, 3)
-    _need(v, "out[1]", _BF16, dev, 3)
-    if k.shape != v.shape or k.shape[1] != kv.num_kv_heads or k.shape[2] != kv.head_dim:
-        raise ValueError(f"outputs must be [total, {kv.num_kv_heads}, {kv.head_dim}], got {tuple(k.shape)} and "
-                         f"{tuple(v.shape)}")
-    _check("mbe_kv_read_q8", lib.mbe_kv_read_q8(
-        ctypes.byref(kv), _ptr(page_table), page_table.shape[1], _ptr(start_pos), _ptr(lens), batch, max_len,
-        k.shape[0], _ptr(k), _ptr(v), _stream(dev)))
+    rows = _token_rows(k, v, ("out[0]", "out[1]"), kv, index, k_pages.device)
+    status = lib.mbe_kv_read_q8(
+        ctypes.byref(kv), page_table.data_ptr(), page_table.shape[1], start_pos.data_ptr(), lens.data_ptr(), batch,
+        max_len, rows, k.data_ptr(), v.data_ptr(), torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        _check("mbe_kv_read_q8", status)
     return k, v
 
 
@@ -798,42 +818,57 @@ def window_attention_q8(q, k_pages, v_pages, k_scales, v_scales, page_table, pre
     is dealt out on the device by the true lengths."""
     lib = load()
     kv = _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table)
-    dev = k_pages.device
-    _need(q, "q", _BF16, dev, 3)
-    _need(prefix_lens, "prefix_lens", _I32, dev, 1)
-    _need(window_lens, "window_lens", _I32, dev, 1)
-    if q.shape[2] != kv.head_dim:
-        raise ValueError(f"q head_dim {q.shape[2]} != cache head_dim {kv.head_dim}")
-    batch = prefix_lens.shape[0]
-    if window_lens.shape[0] != batch or page_table.shape[0] != batch:
+    index, dev = k_pages.get_device(), k_pages.device
+    try:
+        total, hq, d = shape = q.shape
+        (batch,) = batches = prefix_lens.shape
+        usual = (q.dtype is _BF16 and prefix_lens.dtype is _I32 and window_lens.dtype is _I32 and d == kv.head_dim
+                 and window_lens.shape == batches and page_table.shape[0] == batch and q.get_device() == index
+                 and prefix_lens.get_device() == index and window_lens.get_device() == index and q.is_contiguous()
+                 and prefix_lens.is_contiguous() and window_lens.is_contiguous()
+                 and (out is None or (out.dtype is _BF16 and out.shape == shape and out.get_device() == index
+                                      and out.is_contiguous())))
+    except (AttributeError, ValueError):
+        usual = False
+    if not usual:
+        _need(q, "q", _BF16, dev, 3)
+        _need(prefix_lens, "prefix_lens", _I32, dev, 1)
+        _need(window_lens, "window_lens", _I32, dev, 1)
+        if q.shape[2] != kv.head_dim:
+            raise ValueError(f"q head_dim {q.shape[2]} != cache head_dim {kv.head_dim}")
+        if out is not None:
+            _need(out, "out", _BF16, dev, 3)
+            if out.shape != q.shape:
+                raise ValueError("out must have the shape of q")
         raise ValueError("page_table, prefix_lens and window_lens disagree on the batch size")
     if out is None:
         out = torch.empty_like(q)
-    else:
-        _need(out, "out", _BF16, dev, 3)
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
     if max_prefix_len is None:
         host = _host_i32(prefix_lens.cpu() if host_prefix_lens is None else host_prefix_lens, batch, "host_prefix_lens")
         max_prefix_len = int(host.max()) if batch else 0
     if max_window_len is None:
         host = _host_i32(window_lens.cpu() if host_window_lens is None else host_window_lens, batch, "host_window_lens")
         max_window_len = int(host.max()) if batch else 0
-    nblk = int(max_window_len) // int(block_size) if int(block_size) > 0 else 0
-    _flags_gate(block_flags, (batch, nblk), run_if_nonzero, dev)
-    opts = AttnOpts(batch, q.shape[1], page_table.shape[1], q.shape[0], int(max_prefix_len), int(max_window_len),
+    block_size = int(block_size)
+    if block_flags is not None or run_if_nonzero is not None:
+        nblk = int(max_window_len) // block_size if block_size > 0 else 0
+        _flags_gate(block_flags, (batch, nblk), run_if_nonzero, dev)
+    opts = AttnOpts(batch, hq, page_table.shape[1], total, int(max_prefix_len), int(max_window_len),
                     MASK_MODES[mask_mode] if isinstance(mask_mode, str) else int(mask_mode),
-                    float(softmax_scale or 0.0), int(kv_split_tokens), None, None, None, 0, _stream(dev),
-                    _ptr(block_flags), _ptr(run_if_nonzero))
+                    float(softmax_scale or 0.0), int(kv_split_tokens), None, None, None, 0,
+                    torch._C._cuda_getCurrentRawStream(index), _ptr(block_flags), _ptr(run_if_nonzero))
+    args = (q.data_ptr(), ctypes.byref(kv), page_table.data_ptr(), prefix_lens.data_ptr(), window_lens.data_ptr(),
+            block_size, out.data_ptr(), ctypes.byref(opts))
 
     def call():
-        return lib.mbe_window_attention_q8(_ptr(q), ctypes.byref(kv), _ptr(page_table), _ptr(prefix_lens),
-                                           _ptr(window_lens), int(block_size), _ptr(out), ctypes.byref(opts))
+        return lib.mbe_window_attention_q8(*args)
 
     def size():
         return lib.mbe_window_attention_q8_workspace_size(ctypes.byref(kv), ctypes.byref(opts))
 
-    _check("mbe_window_attention_q8", _call_with_workspace(call, size, opts, dev, workspace, "attn_q8"))
+    status = _call_with_workspace(call, size, opts, dev, workspace, "attn_q8")
+    if status:
+        _check("mbe_window_attention_q8", status)
     return out
 
 
@@ -890,23 +925,31 @@ def rotary_turns(frequencies, device):
     return torch.tensor(turns, dtype=torch.int64).to(device)
 
 
-def _rows_of(t, name, device, heads_dim):
-    """Row stride of a [rows, heads, D] tensor whose rows are whole but may lie
-    apart (a slice of a packed projection)."""
+def _rows_of(t, name, index, rows, heads_dim):
+    """Row stride of a bf16 [rows, heads, D] tensor whose rows are whole but may
+    lie apart (a slice of a packed projection)."""
+    try:      # the usual case
+        n, heads, d = t.shape
+        s0, s1, s2 = t.stride()
+        if (t.dtype is _BF16 and t.get_device() == index and s2 == 1 and (s1 == d or heads == 1)
+                and (rows is None or n == rows) and (heads_dim is None or (d == heads_dim[1] and heads_dim[0] in (None, heads)))):
+            return s0 if n > 1 else heads * d
+    except (AttributeError, ValueError):
+        pass
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != _BF16:
         raise TypeError(f"{name} must be {_BF16}, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on GPU {index}, got {t.device}")
     if t.dim() != 3:
         raise ValueError(f"{name} must have 3 dimensions, got {t.dim()}")
-    rows, heads, d = t.shape
-    if heads_dim is not None and (heads, d) != heads_dim:
-        raise ValueError(f"{name} must be [rows, {heads_dim[0]}, {heads_dim[1]}], got {tuple(t.shape)}")
+    n, heads, d = t.shape
+    if (rows is not None and n != rows) or (heads_dim is not None and (d != heads_dim[1] or heads_dim[0] not in (None, heads))):
+        raise ValueError(f"{name} {tuple(t.shape)}: rows, heads or head_dim disagree with q's (k's)")
     if t.numel() and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d)):
         raise ValueError(f"{name}: each row's heads must be contiguous")
-    return t.stride(0) if rows > 1 else heads * d
+    return t.stride(0) if n > 1 else heads * d
 
 
 @_on_device
@@ -921,37 +964,45 @@ def rotary(q, k, start_pos, lens, turns, *, scale=1.0, layout="half", inverse=Fa
     place.  max_len: bound of lens (None: read from the device, a
     synchronisation).  Returns (q, k) rotated, k None if it was."""
     lib = load()
-    dev = q.device
-    q_stride = _rows_of(q, "q", dev, None)
-    rows, hq, d = q.shape
-    hkv, k_stride = 0, 0
-    if k is not None:
-        k_stride = _rows_of(k, "k", dev, None)
-        hkv = k.shape[1]
-        if k.shape[0] != rows or k.shape[2] != d:
-            raise ValueError(f"q and k disagree on rows or head_dim: {tuple(q.shape)} and {tuple(k.shape)}")
-    _need(start_pos, "start_pos", _I32, dev, 1)
-    _need(lens, "lens", _I32, dev, 1)
-    _need(turns, "turns", torch.int64, dev, 1)
-    batch = start_pos.shape[0]
-    if lens.shape[0] != batch:
+    index = q.get_device()
+    try:
+        rows, hq, d = q.shape
+        (batch,) = batches = start_pos.shape
+        (pairs,) = turns.shape
+        usual = (index >= 0 and start_pos.dtype is _I32 and lens.dtype is _I32 and lens.shape == batches
+                 and turns.dtype is torch.int64 and start_pos.get_device() == index and lens.get_device() == index
+                 and turns.get_device() == index and start_pos.is_contiguous() and lens.is_contiguous()
+                 and turns.is_contiguous())
+    except (AttributeError, ValueError):
+        usual = False
+    if not usual:
+        _raw_stream(q.device)          # (refuses anything but a GPU)
+        _rows_of(q, "q", index, None, None)
+        _need(start_pos, "start_pos", _I32, q.device, 1)
+        _need(lens, "lens", _I32, q.device, 1)
+        _need(turns, "turns", torch.int64, q.device, 1)
         raise ValueError("start_pos and lens disagree on the batch size")
-    stream = _stream(dev)
+    q_stride = _rows_of(q, "q", index, None, None)
+    hkv = k_stride = k_out_stride = 0
+    if k is not None:
+        k_stride = _rows_of(k, "k", index, rows, (None, d))
+        hkv = k.shape[1]
     if max_len is None:
         max_len = int(lens.max().item()) if batch else 0
     if out is None:
-        q_out = torch.empty(q.shape, dtype=_BF16, device=dev)
-        k_out = None if k is None else torch.empty(k.shape, dtype=_BF16, device=dev)
+        q_out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+        k_out = None if k is None else torch.empty(k.shape, dtype=_BF16, device=q.device)
     else:
         q_out, k_out = out
         if (k is None) != (k_out is None):
             raise ValueError("out must hold k exactly when k is given")
-    q_out_stride = _rows_of(q_out, "out[0]", dev, (hq, d))
-    k_out_stride = 0 if k is None else _rows_of(k_out, "out[1]", dev, (hkv, d))
-    if q_out.shape[0] != rows or (k is not None and k_out.shape[0] != rows):
-        raise ValueError("outputs must have the rows of the inputs")
-    _check("mbe_rotary", lib.mbe_rotary(
-        _ptr(q), _ptr(q_out), hq, q_stride, q_out_stride, _ptr(k), _ptr(k_out), hkv, k_stride, k_out_stride, d,
-        _ptr(start_pos), _ptr(lens), batch, int(max_len), rows, _ptr(turns), 2 * turns.shape[0],
-        ROTARY_LAYOUTS[layout], float(scale), int(bool(inverse)), stream))
+    q_out_stride = _rows_of(q_out, "out[0]", index, rows, (hq, d))
+    if k is not None:
+        k_out_stride = _rows_of(k_out, "out[1]", index, rows, (hkv, d))
+    status = lib.mbe_rotary(
+        q.data_ptr(), q_out.data_ptr(), hq, q_stride, q_out_stride, _ptr(k), _ptr(k_out), hkv, k_stride, k_out_stride, d,
+        start_pos.data_ptr(), lens.data_ptr(), batch, int(max_len), rows, turns.data_ptr(), 2 * pairs,
+        ROTARY_LAYOUTS[layout], scale, 1 if inverse else 0, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        _check("mbe_rotary", status)
     return q_out, k_out

@@ -274,7 +274,7 @@ def test_the_usual_calls_run_and_wrong_ones_are_named(gpu):
     with pytest.raises(ValueError, match="disagree"):
         gpu.rotary(q, kv[:5], *lens, turns)
     with pytest.raises(ValueError, match="out"):
-        gpu.rotary(q, kv, *lens, turns, out=(q, None))
+        gpu.rotary(q, kv, *lens, turns, max_len=32, out=(q, None))
     with pytest.raises(gpu.MbeError, match="rot_dim"):
         gpu.rotary(q, kv, *lens, turns[:20], max_len=32)
     with pytest.raises(KeyError):
