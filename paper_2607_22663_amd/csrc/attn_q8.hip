@@ -260,19 +260,28 @@ __device__ inline uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, r);
 }
 
-// Q row of this lane as two 8-bit operands per 64 dims; returns the factor that
-// undoes the row's scaling.  `src` null: a row of zeros.
+// This lane's half of a row of Q, as it is (asked for early, turned into operands
+// while the first keys are on their way).  `src` null: zeros.
 template <int D>
-__device__ inline float load_q(const uint16_t *src, i32x8 *hi, i32x8 *lo) {
-  const int h = (threadIdx.x & 63) >> 5;
-  uint4 raw[D / 64][4];
+struct QRow {
+  uint4 v[D / 64][4];
+  __device__ void load(const uint16_t *src) {
+    const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-  for (int s = 0; s < D / 64; ++s)
+    for (int s = 0; s < D / 64; ++s)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      raw[s][j] = uint4{0, 0, 0, 0};
-      if (src) raw[s][j] = *reinterpret_cast<const uint4 *>(src + s * 64 + h * 32 + j * 8);
-    }
+      for (int j = 0; j < 4; ++j) {
+        v[s][j] = uint4{0, 0, 0, 0};
+        if (src) v[s][j] = *reinterpret_cast<const uint4 *>(src + s * 64 + h * 32 + j * 8);
+      }
+  }
+};
+
+// Q row of this lane as two 8-bit operands per 64 dims; returns the factor that
+// undoes the row's scaling.
+template <int D>
+__device__ inline float make_q(const QRow<D> &q, i32x8 *hi, i32x8 *lo) {
+  const auto &raw = q.v;
   float top = 0.f;
 #pragma unroll
   for (int s = 0; s < D / 64; ++s)
@@ -444,6 +453,8 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
         return page_entry(p, u.b, (static_cast<int64_t>(ta) + wave + static_cast<int64_t>(kStreamWaves) * (i + (lane >> 2))) * 4 + (lane & 3));
       };
       int ids = entries(0), ahead[2] = {entries(16), entries(32)};
+      QRow<D> q_row;
+      q_row.load(wanted ? p.q + ((row0 + wi) * p.num_q_heads + u.g * p.group + r % p.group) * D : nullptr);
       auto head_of = [&](int entry) { return static_cast<int64_t>(clamp_page(p, entry)) * p.num_kv_heads + u.g; };
       uint4 kx[2][NB], vx[2][NB];         // tile: [32-key block][chunk of the lane's key], [block][32-dim block]
       auto page_head = [&](int i, int j) { return head_of(__builtin_amdgcn_readlane(ids, (i & 15) * 4 + j)); };
@@ -475,8 +486,7 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
         return h ? b : a;
       };
       i32x8 qh[NS], ql[NS];
-      const float qs = load_q<D>(wanted ? p.q + ((row0 + wi) * p.num_q_heads + u.g * p.group + r % p.group) * D : nullptr, qh, ql);
-      const float cq = qs * p.scale_log2;
+      const float cq = make_q<D>(q_row, qh, ql) * p.scale_log2;
 
       f32x16 acc[NB];
 #pragma unroll
@@ -591,8 +601,8 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
 }
 
 // ------------------------------------------------------- wide kernel
-// Units of 64 * RG rows, RG = 1, 2 or 4: four waves of 64 rows each, one on a
-// SIMD, RG of them side by side on the rows and the others on further key tiles
+// Units of 64 * RG rows, RG = 1 or 2: four waves of 64 rows each, one on a SIMD,
+// RG of them side by side on the rows and the others on further key tiles
 // in turn.  Nothing goes through LDS but the final join of the tiles' groups: each
 // wave loads K and V straight into operand registers, as the streaming kernel
 // does, uses them for both of its 32-row blocks, and waves on the same tile share
@@ -648,6 +658,9 @@ __global__ __launch_bounds__(256, 1) void attn_q8_wide_kernel(AttnQ8Params p) {
         return page_entry(p, u.b, (static_cast<int64_t>(ta) + kg + static_cast<int64_t>(KG) * (i + (lane >> 2))) * 4 + (lane & 3));
       };
       int ids = entries(0), ahead[2] = {entries(16), entries(32)};
+      QRow<D> q_row[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) q_row[b].load(wanted[b] ? p.q + q_at[b] : nullptr);
       auto head_of = [&](int entry) { return static_cast<int64_t>(clamp_page(p, entry)) * p.num_kv_heads + u.g; };
       uint4 kx[2][NB], vx[2][NB];
       auto page_head = [&](int i, int j) { return head_of(__builtin_amdgcn_readlane(ids, (i & 15) * 4 + j)); };
@@ -680,7 +693,7 @@ __global__ __launch_bounds__(256, 1) void attn_q8_wide_kernel(AttnQ8Params p) {
       i32x8 qh[2][NS], ql[2][NS];
       float cq[2];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) cq[b] = load_q<D>(wanted[b] ? p.q + q_at[b] : nullptr, qh[b], ql[b]) * p.scale_log2;
+      for (int b = 0; b < 2; ++b) cq[b] = make_q<D>(q_row[b], qh[b], ql[b]) * p.scale_log2;
 
       f32x16 s0, s1;
       bf16x8 p0[2], p1[2], wv[2][NB];
@@ -868,6 +881,269 @@ __global__ __launch_bounds__(256, 1) void attn_q8_wide_kernel(AttnQ8Params p) {
   } while (deal.next(u));
 }
 
+// ------------------------------------------------------- tile kernel
+// Units of 256 rows: a workgroup of eight waves of 32 rows, two on a SIMD, stages
+// every key tile once in LDS for all of them.
+//
+// K goes into LDS as it is (half the bytes bf16 would take), V as bf16, converted
+// once per workgroup on the way: two planes of 8 keys by dim, 16 bytes each, as
+// P.V's operand reads them.  Rows of K lie in the order of the operand's rows,
+// their 16-byte chunks XOR-swizzled so that any eight rows' equal chunks fall on
+// different banks.
+//
+// A wave works on three 32-key blocks at once, as in the wide kernel.  So
+// iteration t reads K of tiles t and t + 1 and V of t - 1 and t, from three LDS
+// buffers each; it writes K of t + 2 and V of t + 1 from registers, and loads K of
+// t + 4 and V of t + 3 into them: one barrier a tile, two tiles' time for a load.
+constexpr int kTileRows = 256, kTileThreads = 512;
+
+template <int D, int FMT>
+__global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Params p) {
+  constexpr int NB = D / 32, NS = D / 64;
+  constexpr int kChunks = D / 16;         // 16-byte chunks of a K row
+  constexpr int kStagers = 4 * D;         // threads that stage a tile: 16 bytes of K and of V each
+  constexpr int kK = kTile * D, kV = kTile * D * 2;      // bytes of a tile in LDS
+  constexpr int kBuf = kK + kV;
+  __shared__ __align__(16) uint8_t lds[3 * kBuf];
+  __shared__ __align__(16) float sc[3][4][4];            // per page: K scale, log2 and reciprocal of V's
+  if (p.gate && *p.gate == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, h = lane >> 5;
+
+  Deal<kTileRows> deal{p};
+  Piece u;
+  const bool work = deal.start(u);
+  leave_note(p, deal, u, work);
+  if (!work) return;
+  // staging: this thread's 16 bytes of page spage: of K a slot's chunk, of V a dim.
+  // (D = 64: two threads do the same; a branch around the loads would leave the
+  // compiler unsure of how many are in flight, and it would wait for all)
+  const int spage = __builtin_amdgcn_readfirstlane((tid % kStagers) / D), sdim = tid % D;
+  const bool scaler = wave % (D / 64) == 0;              // the wave with dim 0 stages the page's scales
+  const int kslot = sdim / kChunks;
+  const int krow = 32 * (spage >> 1) + 8 * (kslot >> 2) + 4 * (spage & 1) + (kslot & 3);
+  const int k_dst = krow * D + (((sdim % kChunks) ^ (D == 128 ? krow & 7 : (krow >> 1) & 3)) * 16);
+  const int v_dst = kK + (spage * 2 * D + sdim) * 16;
+  // operand reads: 16-byte chunks of the lane's K row (block 0), of its V rows
+  int k_at[2 * NS];
+#pragma unroll
+  for (int i = 0; i < 2 * NS; ++i)
+    k_at[i] = col * D + (((4 * (i >> 1) + 2 * h + (i & 1)) ^ (D == 128 ? col & 7 : (col >> 1) & 3)) * 16);
+  const int v_at = kK + (h * 2 * D + col) * 16;
+
+  do {
+    const int ta = u.ta, tb = u.tb;
+    const int n = u.p + u.w;
+    const int r = u.qt * kTileRows + wave * 32 + col;
+    const bool wanted = row_wanted(p, u.b, u.w, u.row0, r);
+    const bool mine = __builtin_amdgcn_ballot_w64(wanted) != 0;
+    if (!p.block_flags || __syncthreads_or(mine)) {
+      const int wi = r / p.group;
+      const int seen = !wanted ? 0 : (p.causal ? min(n, u.p + (wi / p.block_size + 1) * p.block_size) : n);
+      const int64_t q_at = ((static_cast<int64_t>(u.row0) + wi) * p.num_q_heads + u.g * p.group + r % p.group) * D;
+      const int iters = tb - ta;
+      // Page table entries of this wave's page: lane j of ids holds that of tile
+      // 64 c + j, ahead those of the 64 after.
+      auto entries = [&](int it0) { return page_entry(p, u.b, (static_cast<int64_t>(ta) + it0 + lane) * 4 + spage); };
+      int ids = entries(0), ahead = entries(64);
+      QRow<D> q_row;
+      q_row.load(wanted ? p.q + q_at : nullptr);
+      // (page, head) row of the pools for tile it, asked for in order
+      auto page_head = [&](int it) {
+        return static_cast<int64_t>(clamp_page(p, __builtin_amdgcn_readlane(ids, it & 63))) * p.num_kv_heads + u.g;
+      };
+      struct KRegs {
+        uint4 k;
+        float ks, vs;
+      };
+      auto load_k = [&](KRegs &x, int64_t ph) {
+        x.k = *reinterpret_cast<const uint4 *>(p.k_pages + ph * (kPageSize * D) + sdim * 16);
+        x.ks = p.k_scales[ph];
+        x.vs = p.v_scales[ph];
+      };
+      auto load_v = [&](uint4 &x, int64_t ph) {
+        x = *reinterpret_cast<const uint4 *>(p.v_pages + ph * (kPageSize * D) + sdim * 16);
+      };
+      auto stage_k = [&](const KRegs &x, uint8_t *buf, int sbuf) {
+        *reinterpret_cast<uint4 *>(buf + k_dst) = x.k;
+        if (scaler) {
+          const float vs = v_factor(x.vs);
+          const f32x4 w = {x.ks, __builtin_amdgcn_logf(vs), __builtin_amdgcn_rcpf(vs), 0.f};
+          if (sdim == 0) *reinterpret_cast<f32x4 *>(sc[sbuf][spage]) = w;
+        }
+      };
+      auto stage_v = [&](uint4 x, uint8_t *buf, int it) {
+        const int key = (ta + it) * kTile;
+        if (key + kTile > n) x = zero_behind(x, n - (key + spage * 16));
+        bf16x8 *at = reinterpret_cast<bf16x8 *>(buf + v_dst);
+        at[0] = widen8<FMT>(x.x, x.y);
+        at[D] = widen8<FMT>(x.z, x.w);
+      };
+
+      // tiles 0 and 1 of K, 0 of V in LDS; tiles 2 and 3 of K, 1 and 2 of V on their way
+      KRegs ka, kb;
+      uint4 va, vb;
+      const int64_t ph0 = page_head(0), ph1 = page_head(1), ph2 = page_head(2);
+      int64_t ph = page_head(3);
+      load_k(ka, ph0);
+      load_v(va, ph0);
+      load_k(kb, ph1);
+      load_v(vb, ph1);
+      i32x8 qh[NS], ql[NS];
+      const float cq = make_q<D>(q_row, qh, ql) * p.scale_log2;
+      stage_k(ka, lds, 0);
+      load_k(ka, ph2);
+      stage_v(va, lds, 0);
+      va = vb;
+      load_v(vb, ph2);
+      stage_k(kb, lds + kBuf, 1);
+      load_k(kb, ph);
+
+      f32x16 acc[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) acc[i] = f32x16{};
+      float m = kNegHuge, l = 0.f;
+      f32x16 s0, s1;
+      bf16x8 p0[2], p1[2];
+      p1[0] = p1[1] = bf16x8{};
+      // probabilities of a 32-key block from its scores s; the scores sn of the next
+      // block (kbuf, kblk) and P.V of the one before (pp, vbuf, vblk) beside them
+      auto block = [&](f32x16 &s, f32x16 &sn, const uint8_t *kbuf, int kblk, const bf16x8 (&pp)[2], const uint8_t *vbuf, int vblk,
+                       bf16x8 (&pc)[2], const float *scale, int key0, bool masked) {
+        if (masked) {
+          const int left = seen - (key0 + 16 * h);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = i < left ? s[i] : -__builtin_inff();
+        }
+        const f32x4 w = *reinterpret_cast<const f32x4 *>(scale + 4 * h);
+        uint4 ko[2 * NS];
+        bf16x8 vo[2 * NB];
+#pragma unroll
+        for (int i = 0; i < 2 * NS; ++i) ko[i] = *reinterpret_cast<const uint4 *>(kbuf + k_at[i] + kblk * 32 * D);
+        const bf16x8 *vp = reinterpret_cast<const bf16x8 *>(vbuf + v_at) + vblk * 4 * D;
+        __builtin_amdgcn_sched_barrier(0);
+        const float c = k_factor(w[0], cq);
+        float off = w[1] - m, sum, e[16], t[2] = {0.f, 0.f};
+        auto value = [&](int i) {
+          e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, off));
+          t[i & 1] += e[i];
+          if (i & 1) {
+            uint4 x = __builtin_bit_cast(uint4, pc[i >> 3]);
+            reinterpret_cast<uint32_t *>(&x)[(i >> 1) & 3] = pack2(e[i - 1], e[i]);
+            pc[i >> 3] = __builtin_bit_cast(bf16x8, x);
+          }
+        };
+        // the vector unit's work between the matrix unit's: the first values while
+        // the operands arrive; V's operands follow K's, not all reads at once
+        constexpr int kMfma = 2 * NS + 2 * NB, kFirst = 16 - kMfma > 4 ? 4 : 16 - kMfma;
+        int v = 0;
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) value(v++);
+        __builtin_amdgcn_sched_barrier(0);
+        sn = f32x16{};
+#pragma unroll
+        for (int i = 0; i < kMfma; ++i) {
+          if (i < 2 * NS) {
+#pragma unroll
+            for (int j = i * NB / NS; j < (i + 1) * NB / NS; ++j) vo[j] = vp[(j / NB) * D + (j % NB) * 32];
+            sn = mfma_qk<FMT>(operand(ko[i & ~1], ko[i | 1]), i & 1 ? ql[i >> 1] : qh[i >> 1], sn);
+          } else {
+            const int j = i - 2 * NS;
+            acc[j % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vo[j], pp[j / NB], acc[j % NB], 0, 0, 0);
+          }
+#pragma unroll
+          for (int j = 0; j < (16 - kFirst) * (i + 1) / kMfma - (16 - kFirst) * i / kMfma; ++j) value(v++);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        sum = (t[0] + t[1]) * w[2];
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
+          raise_reference<NB>(s, c, m, l, acc);
+          off = w[1] - m;
+          t[0] = t[1] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) value(i);
+          sum = (t[0] + t[1]) * w[2];
+        }
+        l += sum;
+      };
+
+      __syncthreads();
+      if (mine) {
+        s0 = f32x16{};
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const i32x8 k = operand(*reinterpret_cast<const uint4 *>(lds + k_at[2 * i]), *reinterpret_cast<const uint4 *>(lds + k_at[2 * i + 1]));
+          s0 = mfma_qk<FMT>(k, qh[i], s0);
+          s0 = mfma_qk<FMT>(k, ql[i], s0);
+        }
+      }
+      // buffers of tiles it, it + 1, it + 2, and of it - 1 (the first P.V adds zeros: any V in place will do)
+      uint8_t *b0 = lds, *b1 = lds + kBuf, *b2 = lds + 2 * kBuf, *prev = lds;
+      int i0 = 0, i1 = 1, i2 = 2;
+      auto iteration = [&](int it, KRegs &kr, uint4 &vr) {
+        const int key = (ta + it) * kTile;
+        const bool masked = key + kTile > u.p;
+        if (mine) block(s0, s1, b0, 1, p1, prev, 1, p0, sc[i0][0], key, masked);
+        stage_v(vr, b1, it + 1);
+        load_v(vr, ph);                     // tile it + 3
+        if (mine) block(s1, s0, b1, 0, p0, b0, 0, p1, sc[i0][2], key + 32, masked);
+        stage_k(kr, b2, i2);
+        if (((it + 4) & 63) == 0) {
+          ids = ahead;
+          ahead = entries(it + 4 + 64);
+        }
+        ph = page_head(it + 4);
+        __syncthreads();
+        load_k(kr, ph);                     // tile it + 4
+        prev = b0;
+        b0 = b1;
+        b1 = b2;
+        b2 = prev;
+        const int i = i0;
+        i0 = i1;
+        i1 = i2;
+        i2 = i;
+      };
+      int it = 0;
+      for (; it + 1 < iters; it += 2) {
+        iteration(it, ka, va);
+        iteration(it + 1, kb, vb);
+      }
+      if (it < iters) iteration(it, ka, va);
+      if (mine) {
+        const bf16x8 *vp = reinterpret_cast<const bf16x8 *>(prev + v_at) + 4 * D;
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i)
+          acc[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[(i / NB) * D + (i % NB) * 32], p1[i / NB], acc[i % NB], 0, 0, 0);
+      }
+      l = across_halves_add(l);
+      if (ta > 0 || tb < u.tiles) {
+        const int64_t at = deal.slot() * kTileRows + wave * 32 + col;
+        if (h == 0) {
+          p.part_ml[at * 2] = m;
+          p.part_ml[at * 2 + 1] = l;
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+            *reinterpret_cast<f32x4 *>(p.part_o + at * D + j * 32 + 8 * a + 4 * h) =
+                f32x4{acc[j][4 * a], acc[j][4 * a + 1], acc[j][4 * a + 2], acc[j][4 * a + 3]};
+      } else if (wanted) {
+        const float inv = 1.f / l;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+            *reinterpret_cast<uint2 *>(p.out + q_at + j * 32 + 8 * a + 4 * h) =
+                uint2{pack2(acc[j][4 * a] * inv, acc[j][4 * a + 1] * inv), pack2(acc[j][4 * a + 2] * inv, acc[j][4 * a + 3] * inv)};
+      }
+      __syncthreads();
+    }
+  } while (deal.next(u));
+}
+
 // ------------------------------------------------------------- the join
 // Workgroup x joins the unit that the note of share x + 1 names, if it names one.
 // A block takes RPB rows of it; a row's dims lie across D / 4 lanes, and its parts
@@ -962,7 +1238,7 @@ hipError_t launch(const AttnQ8Params &p, const AttnQ8Plan &plan, hipStream_t str
     e = hipGetLastError();
     if (e == hipSuccess && join) launch_join<D, 128>(p, stream);
   } else {
-    hipLaunchKernelGGL((attn_q8_wide_kernel<D, FMT, 4>), grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((attn_q8_tile_kernel<D, FMT>), grid, dim3(kTileThreads), 0, stream, p);
     e = hipGetLastError();
     if (e == hipSuccess && join) launch_join<D, 256>(p, stream);
   }
