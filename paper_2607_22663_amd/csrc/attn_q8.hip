@@ -1007,24 +1007,25 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Par
       f32x16 s0, s1;
       bf16x8 p0[2], p1[2];
       p1[0] = p1[1] = bf16x8{};
+      // Operands of the next scores and the page factors of the next block: read from
+      // LDS while the block before is worked on.
+      uint4 ko[2 * NS];
+      f32x4 w;
+      auto read_k = [&](const uint8_t *buf, int blk, int i) { ko[i] = *reinterpret_cast<const uint4 *>(buf + k_at[i] + blk * 32 * D); };
+      auto read_w = [&](int buf, int blk) { w = *reinterpret_cast<const f32x4 *>(&sc[buf][2 * blk + h][0]); };
       // probabilities of a 32-key block from its scores s; the scores sn of the next
-      // block (kbuf, kblk) and P.V of the one before (pp, vbuf, vblk) beside them
-      auto block = [&](f32x16 &s, f32x16 &sn, const uint8_t *kbuf, int kblk, const bf16x8 (&pp)[2], const uint8_t *vbuf, int vblk,
-                       bf16x8 (&pc)[2], const float *scale, int key0, bool masked) {
+      // block (from ko) and P.V of the one before (pp, vbuf, vblk) beside them
+      auto block = [&](f32x16 &s, f32x16 &sn, const bf16x8 (&pp)[2], const uint8_t *vbuf, int vblk, bf16x8 (&pc)[2], int key0,
+                       bool masked, const uint8_t *kbuf, int kblk, int wbuf, int wblk) {
         if (masked) {
           const int left = seen - (key0 + 16 * h);
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = i < left ? s[i] : -__builtin_inff();
         }
-        const f32x4 w = *reinterpret_cast<const f32x4 *>(scale + 4 * h);
-        uint4 ko[2 * NS];
         bf16x8 vo[2 * NB];
-#pragma unroll
-        for (int i = 0; i < 2 * NS; ++i) ko[i] = *reinterpret_cast<const uint4 *>(kbuf + k_at[i] + kblk * 32 * D);
         const bf16x8 *vp = reinterpret_cast<const bf16x8 *>(vbuf + v_at) + vblk * 4 * D;
-        __builtin_amdgcn_sched_barrier(0);
-        const float c = k_factor(w[0], cq);
-        float off = w[1] - m, sum, e[16], t[2] = {0.f, 0.f};
+        const float c = k_factor(w[0], cq), lv = w[1], iv = w[2];
+        float off = lv - m, sum, e[16], t[2] = {0.f, 0.f};
         auto value = [&](int i) {
           e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, off));
           t[i & 1] += e[i];
@@ -1034,36 +1035,38 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Par
             pc[i >> 3] = __builtin_bit_cast(bf16x8, x);
           }
         };
-        // the vector unit's work between the matrix unit's: the first values while
-        // the operands arrive; V's operands follow K's, not all reads at once
-        constexpr int kMfma = 2 * NS + 2 * NB, kFirst = 16 - kMfma > 4 ? 4 : 16 - kMfma;
-        int v = 0;
-#pragma unroll
-        for (int i = 0; i < kFirst; ++i) value(v++);
+        // the vector unit's work, and the reads, between the matrix unit's
+        constexpr int kQ = 2 * NS, kP = 2 * NB;
         __builtin_amdgcn_sched_barrier(0);
         sn = f32x16{};
 #pragma unroll
-        for (int i = 0; i < kMfma; ++i) {
-          if (i < 2 * NS) {
+        for (int i = 0; i < kQ; ++i) {
 #pragma unroll
-            for (int j = i * NB / NS; j < (i + 1) * NB / NS; ++j) vo[j] = vp[(j / NB) * D + (j % NB) * 32];
-            sn = mfma_qk<FMT>(operand(ko[i & ~1], ko[i | 1]), i & 1 ? ql[i >> 1] : qh[i >> 1], sn);
-          } else {
-            const int j = i - 2 * NS;
-            acc[j % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vo[j], pp[j / NB], acc[j % NB], 0, 0, 0);
-          }
+          for (int j = i * NB / NS; j < (i + 1) * NB / NS; ++j) vo[j] = vp[(j / NB) * D + (j % NB) * 32];
+          sn = mfma_qk<FMT>(operand(ko[i & ~1], ko[i | 1]), i & 1 ? ql[i >> 1] : qh[i >> 1], sn);
 #pragma unroll
-          for (int j = 0; j < (16 - kFirst) * (i + 1) / kMfma - (16 - kFirst) * i / kMfma; ++j) value(v++);
+          for (int j = 8 * i / kQ; j < 8 * (i + 1) / kQ; ++j) value(j);
           __builtin_amdgcn_sched_barrier(0);
         }
-        sum = (t[0] + t[1]) * w[2];
+#pragma unroll
+        for (int i = 0; i < kP; ++i) {
+          if (i >= kP / 2) {
+            if (i == kP / 2) read_w(wbuf, wblk);
+            read_k(kbuf, kblk, i - kP / 2);
+          }
+          acc[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vo[i], pp[i / NB], acc[i % NB], 0, 0, 0);
+#pragma unroll
+          for (int j = 8 + 8 * i / kP; j < 8 + 8 * (i + 1) / kP; ++j) value(j);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        sum = (t[0] + t[1]) * iv;
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit)) != 0, 0)) {
           raise_reference<NB>(s, c, m, l, acc);
-          off = w[1] - m;
+          off = lv - m;
           t[0] = t[1] = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) value(i);
-          sum = (t[0] + t[1]) * w[2];
+          sum = (t[0] + t[1]) * iv;
         }
         l += sum;
       };
@@ -1077,6 +1080,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Par
           s0 = mfma_qk<FMT>(k, qh[i], s0);
           s0 = mfma_qk<FMT>(k, ql[i], s0);
         }
+#pragma unroll
+        for (int i = 0; i < 2 * NS; ++i) read_k(lds, 1, i);
+        read_w(0, 0);
       }
       // buffers of tiles it, it + 1, it + 2, and of it - 1 (the first P.V adds zeros: any V in place will do)
       uint8_t *b0 = lds, *b1 = lds + kBuf, *b2 = lds + 2 * kBuf, *prev = lds;
@@ -1084,10 +1090,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Par
       auto iteration = [&](int it, KRegs &kr, uint4 &vr) {
         const int key = (ta + it) * kTile;
         const bool masked = key + kTile > u.p;
-        if (mine) block(s0, s1, b0, 1, p1, prev, 1, p0, sc[i0][0], key, masked);
+        if (mine) block(s0, s1, p1, prev, 1, p0, key, masked, b1, 0, i0, 1);
         stage_v(vr, b1, it + 1);
         load_v(vr, ph);                     // tile it + 3
-        if (mine) block(s1, s0, b1, 0, p0, b0, 0, p1, sc[i0][2], key + 32, masked);
+        if (mine) block(s1, s0, p0, b0, 0, p1, key + 32, masked, b1, 1, i1, 0);
         stage_k(kr, b2, i2);
         if (((it + 4) & 63) == 0) {
           ids = ahead;
