@@ -137,10 +137,26 @@ mbe::KvQ8Params range_params(const mbe_paged_kv_q8 *kv, const int32_t *page_tabl
 }
 
 // --------------------------------------------------------------- attention
-// Shares of the work: one workgroup of eight waves, or two of four, on each of
-// the 256 CUs.
-constexpr int64_t kStreamWgs = 512, kTileWgs = 256;
-constexpr int32_t kMinTiles = 8;
+// Shares of the work: one workgroup on each of the 256 CUs.  (Two of the streaming
+// kernel, main kernel: one token of 32 sequences of 1000 to 8192 37 against 33 us,
+// of 32 x 65536 381 against 355.)
+constexpr int64_t kWgs = 256;
+// Smallest share where units are cut.  1 x 8192 / 8 x 2048 keys, us, with shares of
+// at least 2 / 4 / 8 tiles: one token 13.4 12.9 12.9 / 13.2 13.1 12.7, windows of 32
+// 33 29 28 / 28 28 29, of 64 37 37 37 / 36 36 38; 1 x 1024, windows of 64 22 23 29.
+constexpr int32_t kMinTiles = 4;
+// Tiles' time that beginning a unit takes a workgroup (q, the first pages, the
+// result).  Main kernel, us, at 0 / 4 / 8 / 12: one token of 32 sequences of 1000
+// to 8192 39 / 37 / 37 / 37, blocks behind 8 x 16384 65 / 61 / 59 / 57, 12 ragged
+// windows behind 1000 to 12000 132 / 123 / 120 / 121, windows of 128 behind 64 x
+// 4096 to 32768 1204 / 1174 / 1154 / 1146.
+constexpr int32_t kStartTiles = 8;
+// By units of 32, of 64 and 128, of 256 rows.  A workgroup alone takes 0.29, 0.88,
+// 1.46 us a tile (D = 128), the memory 2.8 ns; parts cost about 5 us to join.
+constexpr int32_t kMemoryTiles[3] = {100, 300, 500};
+constexpr int32_t kJoinTiles[3] = {8, 4, 2};
+// Longest units that are not cut at all, without a look at the lengths: one kernel.
+constexpr int32_t kWholeTiles[3] = {16, 8, 8};
 
 mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int32_t block_size, mbe::AttnQ8Plan *pl) {
   const mbe_status st = check_pool(kv);
@@ -171,7 +187,7 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
   *pl = mbe::AttnQ8Plan{};
   const int64_t seq_rows = group * o->max_window_len;
   pl->rows = seq_rows <= 32 ? 32 : seq_rows <= 64 ? 64 : seq_rows <= 128 ? 128 : 256;
-  const int64_t most_wgs = pl->rows == 32 ? kStreamWgs : kTileWgs;
+  const int form = pl->rows == 32 ? 0 : pl->rows <= 128 ? 1 : 2;
   const int64_t qtiles = (seq_rows + pl->rows - 1) / pl->rows;
   const int64_t tiles = (max_kv + mbe::kKeyTile - 1) / mbe::kKeyTile;
   // units within the bounds: qtiles of every sequence, but no more than the rows fill
@@ -181,14 +197,17 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
   pl->qtiles = static_cast<int32_t>(std::max<int64_t>(1, qtiles));
   pl->min_tiles = o->kv_split_tokens > 0 ? o->kv_split_tokens / mbe::kKeyTile : kMinTiles;
   // (the kernels count the tiles of all units in 32 bits, whatever the lengths within the bounds)
-  pl->split = tiles > pl->min_tiles && grid <= kMaxGrid && grid * tiles < (1LL << 31);
+  pl->start_tiles = kStartTiles;
+  pl->memory_tiles = kMemoryTiles[form];
+  pl->join_tiles = o->kv_split_tokens > 0 ? 0 : kJoinTiles[form];
+  pl->split = tiles > (o->kv_split_tokens > 0 ? pl->min_tiles : kWholeTiles[form]) && grid <= kMaxGrid && grid * (tiles + kStartTiles) < (1LL << 31);
   if (!pl->split && grid > kMaxGrid) return report(MBE_ERR_BAD_SHAPE, "too many sequences, heads and rows for one call");
   if (!pl->split) {
     pl->wgs = static_cast<int32_t>(grid);
     return MBE_OK;
   }
   const int64_t most = units * ((tiles + pl->min_tiles - 1) / pl->min_tiles);
-  pl->wgs = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(most_wgs, most)));
+  pl->wgs = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(kWgs, most)));
   const size_t part_rows = 2 * static_cast<size_t>(pl->wgs) * pl->rows;
   pl->part_o_off = align_up(static_cast<size_t>(pl->wgs) * 8 * sizeof(int32_t));
   pl->part_ml_off = pl->part_o_off + align_up(part_rows * kv->head_dim * sizeof(float));
@@ -315,6 +334,9 @@ mbe_status mbe_window_attention_q8(const void *q, const mbe_paged_kv_q8 *paged_k
   p.gate = o->run_if_nonzero;
   p.wgs = pl.wgs;
   p.min_tiles = pl.min_tiles;
+  p.start_tiles = pl.start_tiles;
+  p.memory_tiles = pl.memory_tiles;
+  p.join_tiles = pl.join_tiles;
   p.qtiles = pl.qtiles;
   p.split = pl.split;
   const hipError_t e = mbe::launch_attn_q8(p, pl, paged_kv->head_dim, paged_kv->format, hs);

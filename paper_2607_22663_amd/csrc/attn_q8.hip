@@ -62,6 +62,15 @@ __device__ inline uint32_t scan_lanes(uint32_t x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
   return x;
 }
+// Largest over the lanes up to this one.
+__device__ inline uint32_t max_lanes(uint32_t x) {
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true)));
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true)));
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true)));
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true)));
+  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false)));
+  return max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false)));
+}
 __device__ inline uint32_t lane_value(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
 // A workgroup's piece of a unit: tiles [ta, tb) of tile range [0, tiles) of row
@@ -70,29 +79,38 @@ struct Piece {
   int b, g, qt, p, w, row0, ta, tb, tiles;
 };
 
-// The line of all units' tiles, cut into shares.  With fewer tiles than the
-// workgroups would take at min_tiles each, units are padded to whole shares of
-// min_tiles, so that a workgroup never has pieces of two units; otherwise every
-// workgroup takes an equal share, across units.  (The launch bounds the line to
-// 32 bits.)
+// The line of all units' tiles, cut into shares.
+//   Few tiles: units are padded to whole shares of min_tiles, so that a workgroup
+//   never has pieces of two units.
+//   Units alike, and no more than workgroups: a unit each, where the longest takes
+//   no longer than equal shares, or than the memory needs for all, and a join.
+//   Otherwise every workgroup takes an equal share, across units.  There a unit has
+//   start_tiles places before its tiles, the time that beginning one takes.
+// (The launch bounds the line to 32 bits.)
 template <int ROWS>
 struct Deal {
   const AttnQ8Params &p;
   uint32_t share, at, end;      // this workgroup's part of the line: [at, end)
-  uint32_t first;               // its begin
+  uint32_t begin, length;       // the unit at hand in the line
+  uint32_t pieces;              // of this workgroup before the one at hand
   bool padded;
 
+  __device__ uint32_t starts() const { return padded ? 0 : p.start_tiles; }
   __device__ uint32_t whole(uint32_t tiles) const {
-    return padded ? (tiles + share - 1) / share * share : tiles;
+    return padded ? (tiles + share - 1) / share * share : tiles + p.start_tiles;
   }
-  __device__ void sequence(int b, int &pl, int &wl, uint32_t &tiles, uint32_t &units) const {
-    pl = wl = 0;
-    if (b < p.batch) {
-      pl = min(max(p.prefix_lens[b], 0), p.max_prefix);
-      wl = min(max(p.window_lens[b], 0), p.max_window);
-    }
-    tiles = (static_cast<uint32_t>(pl) + wl + kTile - 1) / kTile;
-    units = (static_cast<uint32_t>(wl) * p.group + ROWS - 1) / ROWS * p.num_kv_heads;
+  // The lane's sequence b: lengths within the bounds (0 behind the batch).
+  struct Lens {
+    int p, w;
+  };
+  __device__ Lens lens_of(int b) const {
+    Lens s = {0, 0};
+    if (b < p.batch) s = {p.prefix_lens[b], p.window_lens[b]};
+    return {min(max(s.p, 0), p.max_prefix), min(max(s.w, 0), p.max_window)};
+  }
+  __device__ uint32_t tiles_of(Lens s) const { return (static_cast<uint32_t>(s.p) + s.w + kTile - 1) / kTile; }
+  __device__ uint32_t units_of(Lens s) const {
+    return (static_cast<uint32_t>(s.w) * p.group + ROWS - 1) / ROWS * p.num_kv_heads;
   }
 
   // Its first piece; false: it has none.
@@ -103,92 +121,115 @@ struct Deal {
       u.qt = static_cast<int>(blockIdx.x) - rest * p.qtiles;
       u.b = rest / p.num_kv_heads;
       u.g = rest - u.b * p.num_kv_heads;
-      uint32_t rows = 0, tiles = 0, units = 0;
+      uint32_t rows = 0, units = 0;
       for (int b0 = 0; b0 <= u.b; b0 += 64) {
-        int pl, wl;
-        sequence(b0 + lane, pl, wl, tiles, units);
-        const uint32_t up = scan_lanes(wl);
+        const Lens s = lens_of(b0 + lane);
+        const uint32_t up = scan_lanes(s.w);
         if (u.b < b0 + 64) {
           const int l = u.b - b0;
-          u.p = lane_value(pl, l);
-          u.w = lane_value(wl, l);
-          u.tiles = lane_value(tiles, l);
+          u.p = lane_value(s.p, l);
+          u.w = lane_value(s.w, l);
+          u.tiles = lane_value(tiles_of(s), l);
           u.row0 = rows + lane_value(up, l) - u.w;
-          units = lane_value(units, l);
+          units = lane_value(units_of(s), l);
         }
         rows += lane_value(up, 63);
       }
       u.ta = 0;
       u.tb = u.tiles;
-      at = end = 0;
+      at = end = pieces = 0;
       return u.qt * p.num_kv_heads < static_cast<int>(units);
     }
-    uint32_t tight = 0, loose = 0;
+    uint32_t tight = 0, loose = 0, count = 0, longest = 0;
     padded = true;
     share = p.min_tiles;
+    Lens s{};
     for (int b0 = 0; b0 < p.batch; b0 += 64) {
-      int pl, wl;
-      uint32_t tiles, units;
-      sequence(b0 + lane, pl, wl, tiles, units);
-      tight += lane_value(scan_lanes(tiles * units), 63);
+      s = lens_of(b0 + lane);
+      const uint32_t tiles = tiles_of(s), units = units_of(s);
+      tight += lane_value(scan_lanes((tiles + p.start_tiles) * units), 63);
       loose += lane_value(scan_lanes(whole(tiles) / share * units), 63);     // in shares
+      count += lane_value(scan_lanes(units), 63);
+      longest = max(longest, lane_value(max_lanes(units ? tiles : 0), 63));
     }
     padded = loose <= static_cast<uint32_t>(p.wgs);
-    if (!padded) share = max(share, (tight + p.wgs - 1) / p.wgs);
+    const uint32_t even = max(share, padded ? 0 : (tight + p.wgs - 1) / p.wgs);
+    if (count <= static_cast<uint32_t>(p.wgs) && longest <= max(even, tight / p.memory_tiles) + p.join_tiles) {
+      padded = true;
+      share = longest;
+      loose = count;
+    } else if (!padded) {
+      share = even;
+    }
     const uint32_t total = padded ? loose * share : tight;
-    first = at = share * blockIdx.x;
+    at = share * blockIdx.x;
     end = min(at + share, total);
-    if (blockIdx.x > (total - 1) / share || total == 0) return false;
-    piece(u);
+    pieces = 0;
+    if (total == 0 || blockIdx.x > (total - 1) / share) return false;      // (share > 0 where total is)
+    if (p.batch <= 64) {
+      uint32_t base = 0, rows = 0;
+      in_chunk(u, 0, s, base, rows);
+    } else {
+      piece(u);
+    }
+    return u.ta < u.tb || next(u);
+  }
+
+  // Whether `at` lies in the 64 sequences from b0 on (the lanes hold their lengths);
+  // the piece there.  base, rows: places and rows before them, moved past them if not.
+  __device__ bool in_chunk(Piece &u, int b0, Lens s, uint32_t &base, uint32_t &rows) {
+    const uint32_t tiles = tiles_of(s), units = units_of(s);
+    const uint32_t own = whole(tiles) * units, up = scan_lanes(own), wup = scan_lanes(s.w);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(base + up > at);
+    if (!past) {
+      base += lane_value(up, 63);
+      rows += lane_value(wup, 63);
+      return false;
+    }
+    const int l = __builtin_ctzll(past);
+    u.b = b0 + l;
+    u.p = lane_value(s.p, l);
+    u.w = lane_value(s.w, l);
+    u.tiles = lane_value(tiles, l);
+    u.row0 = rows + lane_value(wup, l) - u.w;
+    const uint32_t from = base + lane_value(up, l) - lane_value(own, l);
+    const uint32_t qtiles = lane_value(units, l) / p.num_kv_heads;
+    length = whole(u.tiles);
+    const uint32_t unit = (at - from) / length;
+    u.g = unit / qtiles;
+    u.qt = unit - u.g * qtiles;
+    begin = from + unit * length;
+    const uint32_t first = begin + starts();       // its tile 0
+    u.ta = at > first ? at - first : 0;
+    u.tb = min(static_cast<uint32_t>(u.tiles), end > first ? end - first : 0);
     return true;
   }
 
   // The piece at `at`.
   __device__ void piece(Piece &u) {
-    const int lane = threadIdx.x & 63;
     uint32_t base = 0, rows = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 64) {
-      int pl, wl;
-      uint32_t tiles, units;
-      sequence(b0 + lane, pl, wl, tiles, units);
-      const uint32_t own = whole(tiles) * units, up = scan_lanes(own), wup = scan_lanes(wl);
-      const uint64_t past = __builtin_amdgcn_ballot_w64(base + up > at);
-      if (past) {
-        const int l = __builtin_ctzll(past);
-        u.b = b0 + l;
-        u.p = lane_value(pl, l);
-        u.w = lane_value(wl, l);
-        u.tiles = lane_value(tiles, l);
-        u.row0 = rows + lane_value(wup, l) - u.w;
-        const uint32_t rel = at - (base + lane_value(up, l) - lane_value(own, l));
-        const uint32_t length = whole(u.tiles), unit = rel / length, qtiles = lane_value(units, l) / p.num_kv_heads;
-        u.g = unit / qtiles;
-        u.qt = unit - u.g * qtiles;
-        u.ta = rel - unit * length;
-        u.tb = min(static_cast<uint32_t>(u.tiles), u.ta + (end - at));
-        return;
-      }
-      base += lane_value(up, 63);
-      rows += lane_value(wup, 63);
-    }
+    for (int b0 = 0; b0 < p.batch; b0 += 64)
+      if (in_chunk(u, b0, lens_of(b0 + static_cast<int>(threadIdx.x & 63)), base, rows)) return;
   }
 
-  // The next piece of its share; false: it has no more.
+  // The next piece of its share; false: it has no more.  (A share may end before a
+  // unit's first tile.)
   __device__ bool next(Piece &u) {
     if (!p.split || padded) return false;
-    at += u.tb - u.ta;
+    if (u.ta < u.tb) ++pieces;
+    at = begin + length;
     if (at >= end) return false;
     piece(u);
-    return true;
+    return u.ta < u.tb;
   }
 
   // Slot of the partial result of the piece at hand: a share has at most two, its
   // first piece and its last.
-  __device__ int64_t slot() const { return 2 * static_cast<int64_t>(blockIdx.x) + (at == first ? 0 : 1); }
+  __device__ int64_t slot() const { return 2 * static_cast<int64_t>(blockIdx.x) + (pieces == 0 ? 0 : 1); }
 };
 
-// What the join kernel is told by the workgroup whose share begins at a unit's
-// first border: the unit's parts lie in slots slot, 2 wg, 2 wg + 2, ...
+// What the join kernel is told by the workgroup with a unit's second part: the
+// parts lie in slots slot, 2 wg, 2 wg + 2, ...
 struct JoinNote {
   int32_t parts;            // 0: nothing to join here
   int32_t b, g, qt, w, row0, slot, unused;
@@ -199,16 +240,19 @@ __device__ inline void leave_note(const AttnQ8Params &p, const Deal<ROWS> &d, co
   if (!p.split || threadIdx.x != 0) return;
   JoinNote n{};
   const uint32_t wg = blockIdx.x;
-  if (any && u.ta > 0 && static_cast<uint32_t>(u.ta) <= d.share) {
-    // shares after this one that the unit reaches into
-    const uint32_t left = static_cast<uint32_t>(u.tiles - u.ta);
-    n.parts = 1 + static_cast<int32_t>((left + d.share - 1) / d.share);
-    n.b = u.b;
-    n.g = u.g;
-    n.qt = u.qt;
-    n.w = u.w;
-    n.row0 = u.row0;
-    n.slot = static_cast<int32_t>(2 * (wg - 1) + (static_cast<uint32_t>(u.ta) == d.share ? 0 : 1));
+  if (any && u.ta > 0) {
+    // the shares with the unit's first and last tile; the first holds it second
+    // where the share begins in the unit before
+    const uint32_t w0 = (d.begin + d.starts()) / d.share, w1 = (d.begin + d.length - 1) / d.share;
+    if (wg == w0 + 1) {
+      n.parts = static_cast<int32_t>(w1 - w0 + 1);
+      n.b = u.b;
+      n.g = u.g;
+      n.qt = u.qt;
+      n.w = u.w;
+      n.row0 = u.row0;
+      n.slot = static_cast<int32_t>(2 * w0 + (w0 * d.share < d.begin ? 1 : 0));
+    }
   }
   *reinterpret_cast<JoinNote *>(p.notes + 8 * static_cast<int64_t>(wg)) = n;
 }
@@ -1222,8 +1266,10 @@ __global__ __launch_bounds__(256) void attn_q8_join_kernel(AttnQ8Params p) {
 template <int D, int ROWS>
 void launch_join(const AttnQ8Params &p, hipStream_t stream) {
   constexpr int kRows = ROWS <= 32 ? 2 : 256 / (D / 4);
-  hipLaunchKernelGGL((attn_q8_join_kernel<D, ROWS, kRows>), dim3(static_cast<unsigned>(p.wgs - 1), ROWS / kRows), dim3(256),
-                     0, stream, p);
+  const int rows = static_cast<int>(min(static_cast<int64_t>(ROWS), static_cast<int64_t>(p.group) * p.max_window));
+  hipLaunchKernelGGL((attn_q8_join_kernel<D, ROWS, kRows>),
+                     dim3(static_cast<unsigned>(p.wgs - 1), static_cast<unsigned>((rows + kRows - 1) / kRows)), dim3(256), 0,
+                     stream, p);
 }
 
 template <int D, int FMT>

@@ -63,6 +63,9 @@ struct AttnQ8Params {
   const int32_t *gate;               // device int32 or null: nothing is done when *gate == 0
   int32_t wgs;                       // workgroups
   int32_t min_tiles;                 // fewest 64-key tiles of a workgroup's share
+  int32_t start_tiles;               // tiles' time that beginning a unit takes
+  int32_t memory_tiles;              // tiles the memory delivers in a workgroup's time for one
+  int32_t join_tiles;                // tiles' time that joining parts takes
   int32_t qtiles;                    // row tiles of the widest window
   int32_t split;                     // 0: a workgroup takes one whole unit
 };
@@ -70,7 +73,7 @@ struct AttnQ8Params {
 // Launch shape of the attention, from host-known bounds.
 struct AttnQ8Plan {
   int32_t rows;       // packed query rows of a unit
-  int32_t qtiles, wgs, min_tiles, split;
+  int32_t qtiles, wgs, min_tiles, start_tiles, memory_tiles, join_tiles, split;
   size_t part_o_off, part_ml_off, bytes;
 };
 hipError_t launch_attn_q8(const AttnQ8Params &p, const AttnQ8Plan &plan, int head_dim, int format, hipStream_t stream);
