@@ -63,8 +63,9 @@ typedef struct {
  *   s           smallest power of two, in [2^-100, 2^120], with
  *               amax / s <= the type's largest finite value
  *   scale       s, or max(s, old scale) where a slot is kept
- *   new value   x / scale, rounded to the nearest 8-bit value (ties to even);
- *               +-inf becomes the largest finite value, NaN stays NaN
+ *   new value   x / scale (in fp32: exact for powers of two), rounded to the
+ *               nearest 8-bit value, ties to even; +-inf becomes the largest
+ *               finite value, NaN stays NaN
  *   kept value  old value * (old scale / scale), rounded likewise
  * The remaining slots keep their bytes.  kv_lens (device int32 [batch], NULL =
  * start_pos): tokens the sequence holds before the call.  An append passes
@@ -83,9 +84,9 @@ mbe_status mbe_kv_write_q8(const mbe_paged_kv_q8 *paged_kv, const int32_t *page_
 
 /* Read-back: the tokens at positions start_pos[b] .. start_pos[b] + lens[b] - 1
  * of every sequence as bf16 [total_tokens][num_kv_heads][head_dim], rows as in
- * mbe_kv_write_q8.  Each value is the 8-bit value times its scale, rounded
- * once (exact for the scales mbe_kv_write_q8 stores, above bf16's smallest
- * normal value).  Tokens whose table slot or page id is out of range read as
+ * mbe_kv_write_q8.  Each value is the 8-bit value times its scale, in fp32,
+ * rounded to bf16 (exact for the scales mbe_kv_write_q8 stores, down to bf16's
+ * smallest normal value).  Tokens whose table slot or page id is out of range read as
  * zeros; rows behind the last sequence are left as they were. */
 mbe_status mbe_kv_read_q8(const mbe_paged_kv_q8 *paged_kv, const int32_t *page_table, int32_t max_pages_per_seq,
                           const int32_t *start_pos, const int32_t *lens, int32_t batch, int32_t max_len,
@@ -96,11 +97,16 @@ mbe_status mbe_kv_read_q8(const mbe_paged_kv_q8 *paged_kv, const int32_t *page_t
  * read differently:
  *   kv_split_tokens  the fewest keys that a workgroup takes of a sequence
  *                    before the sequence is split further; 0 lets the library
- *                    choose; otherwise a positive multiple of 64
- *   host_prefix_lens, host_window_lens   not needed: the work is dealt out on
- *                    the device, from the device lengths
+ *                    choose (and take smaller tiles of rows where there is
+ *                    little to do); otherwise a positive multiple of 64
+ *   host_prefix_lens, host_window_lens   not read: the work is dealt out on the
+ *                    device, from the device lengths
  * q and the probabilities take part in full bf16 precision; the cache's values
- * are never rounded again; accumulation is fp32.  Deterministic. */
+ * are never rounded again; accumulation is fp32.  Deterministic: the same
+ * inputs and bounds give bitwise the same outputs.
+ * A row of q that holds an infinity or a NaN gives NaN, in that row alone.
+ * V values that a row's scope hides within a sequence's own tokens (block-causal
+ * windows) must be finite, as must the scales of all covered pages. */
 mbe_status mbe_window_attention_q8(const void *q, const mbe_paged_kv_q8 *paged_kv, const int32_t *page_table,
                                    const int32_t *prefix_lens, const int32_t *window_lens, int32_t block_size,
                                    void *out, const mbe_attn_opts *opts);

@@ -151,6 +151,14 @@ constexpr int32_t kMinTiles = 4;
 // windows behind 1000 to 12000 132 / 123 / 120 / 121, windows of 128 behind 64 x
 // 4096 to 32768 1204 / 1174 / 1154 / 1146.
 constexpr int32_t kStartTiles = 8;
+// Units of 32 rows for any window while there is little to do, in tiles (and
+// starts) of such units: they begin in half the time, and spread wider.  us with
+// units of 32 rows / the best of 64 to 256, by that number: windows of 32, 8 x 64
+// (1300) 7.5 / 11, 8 x 512 (2200) 11 / 21, 8 x 2048 (5200) 23 / 28, 32 x 512 (8700)
+// 19 / 23, 8 x 8192 (17500) 51 / 40; of 16, 32 x 2048 (10500) 30 / 37; of 64, 8 x
+// 2048 (10500) 30 / 34, 32 x 64 (10200) 19 / 16, 8 x 8192 (35000) 85 / 59; of 256,
+// 1 x 2048 (5600) 21 / 26, 1 x 8192 (17900) 50 / 40.
+constexpr int64_t kLittleWork = 11000;
 // By units of 32, of 64 and 128, of 256 rows.  A workgroup alone takes 0.29, 0.88,
 // 1.46 us a tile (D = 128), the memory 2.8 ns; parts cost about 5 us to join.
 constexpr int32_t kMemoryTiles[3] = {100, 300, 500};
@@ -186,13 +194,18 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
 
   *pl = mbe::AttnQ8Plan{};
   const int64_t seq_rows = group * o->max_window_len;
-  pl->rows = seq_rows <= 32 ? 32 : seq_rows <= 64 ? 64 : seq_rows <= 128 ? 128 : 256;
+  const int64_t tiles = (max_kv + mbe::kKeyTile - 1) / mbe::kKeyTile;
+  // units of `rows` rows within the bounds: no more than the rows fill
+  auto units_of = [&](int64_t rows) {
+    const int64_t each = (seq_rows + rows - 1) / rows;
+    const int64_t all = std::min<int64_t>(o->batch * each, o->total_q * group / rows + o->batch);
+    return std::max<int64_t>(1, all * kv->num_kv_heads);
+  };
+  const bool little = o->kv_split_tokens == 0 && units_of(32) <= kLittleWork / (tiles + kStartTiles);
+  pl->rows = seq_rows <= 32 || little ? 32 : seq_rows <= 64 ? 64 : seq_rows <= 128 ? 128 : 256;
   const int form = pl->rows == 32 ? 0 : pl->rows <= 128 ? 1 : 2;
   const int64_t qtiles = (seq_rows + pl->rows - 1) / pl->rows;
-  const int64_t tiles = (max_kv + mbe::kKeyTile - 1) / mbe::kKeyTile;
-  // units within the bounds: qtiles of every sequence, but no more than the rows fill
-  const int64_t seq_units = std::min<int64_t>(o->batch * qtiles, o->total_q * group / pl->rows + o->batch);
-  const int64_t units = std::max<int64_t>(1, seq_units * kv->num_kv_heads);
+  const int64_t units = units_of(pl->rows);
   const int64_t grid = std::max<int64_t>(1, o->batch * qtiles * kv->num_kv_heads);
   pl->qtiles = static_cast<int32_t>(std::max<int64_t>(1, qtiles));
   pl->min_tiles = o->kv_split_tokens > 0 ? o->kv_split_tokens / mbe::kKeyTile : kMinTiles;
@@ -200,7 +213,8 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
   pl->start_tiles = kStartTiles;
   pl->memory_tiles = kMemoryTiles[form];
   pl->join_tiles = o->kv_split_tokens > 0 ? 0 : kJoinTiles[form];
-  pl->split = tiles > (o->kv_split_tokens > 0 ? pl->min_tiles : kWholeTiles[form]) && grid <= kMaxGrid && grid * (tiles + kStartTiles) < (1LL << 31);
+  pl->split = tiles > (o->kv_split_tokens > 0 ? pl->min_tiles : kWholeTiles[form]) && grid <= kMaxGrid &&
+              grid * (tiles + kStartTiles) < (1LL << 31);
   if (!pl->split && grid > kMaxGrid) return report(MBE_ERR_BAD_SHAPE, "too many sequences, heads and rows for one call");
   if (!pl->split) {
     pl->wgs = static_cast<int32_t>(grid);

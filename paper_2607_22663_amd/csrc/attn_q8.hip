@@ -37,6 +37,7 @@
 #include <type_traits>
 
 #include "q8.h"
+#include "q8_device.h"
 
 namespace mbe {
 namespace {
@@ -52,27 +53,6 @@ constexpr int kTile = 64;                   // keys of a tile: 4 pages
 constexpr float kNegHuge = -1e30f;
 
 // ------------------------------------------------------------ work dealing
-// Sum over the lanes up to this one, by DPP: within rows of 16, then across.
-__device__ inline uint32_t scan_lanes(uint32_t x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr:1, 2, 4, 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast:15, 31
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
-// Largest over the lanes up to this one.
-__device__ inline uint32_t max_lanes(uint32_t x) {
-  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true)));
-  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true)));
-  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true)));
-  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true)));
-  x = max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false)));
-  return max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false)));
-}
-__device__ inline uint32_t lane_value(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-
 // A workgroup's piece of a unit: tiles [ta, tb) of tile range [0, tiles) of row
 // tile qt of KV head g of sequence b, whose window starts at row row0 of q.
 struct Piece {

@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "q8.h"
+#include "q8_device.h"
 
 namespace mbe {
 namespace {
@@ -168,12 +169,7 @@ __device__ inline bool page_item(const KvQ8Params &p, PageItem *it) {
   it->page = it->start / kPageSize + rel;
   it->pos = it->page * kPageSize;
   if (it->pos >= it->end) return false;
-  // first row of the sequence: the lengths before it, summed across the lanes
-  int64_t row0 = 0;
-  for (int j = threadIdx.x & 63; j < b; j += 64) row0 += min(max(p.lens[j], 0), p.max_len);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) row0 += __shfl_xor(row0, o);
-  it->row = row0 + (it->pos - it->start);
+  it->row = rows_before(p.lens, b, p.max_len) + (it->pos - it->start);
   return true;
 }
 

@@ -16,6 +16,7 @@
 #include <stdint.h>
 
 #include "q8.h"
+#include "q8_device.h"
 
 namespace mbe {
 namespace {
@@ -38,23 +39,16 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   const int len = min(max(p.lens[b], 0), p.max_len);
   const int item = static_cast<int>(blockIdx.x) * 256 + static_cast<int>(threadIdx.x);
   if (static_cast<int>(blockIdx.x) * (256 / kChunks) >= len) return;
-  int64_t row0 = 0;
-  for (int j = threadIdx.x & 63; j < b; j += 64) row0 += min(max(p.lens[j], 0), p.max_len);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) row0 += __shfl_xor(row0, o);
   const int t = item / kChunks, c = item % kChunks;
-  const int64_t row = row0 + t;
+  const int64_t row = rows_before(p.lens, b, p.max_len) + t;
   if (t >= len || row >= p.total_rows) return;
   const int heads = p.num_q_heads + p.num_kv_heads;
   const int h0 = static_cast<int>(blockIdx.z) * HEADS;
+  // The two 8-dim chunks of this thread: c-th of the rotated dims' halves (or of the
+  // other dims' halves), so that neighbours' chunks lie next to each other.
   const int half = p.rot_dim / 2;
   const bool rotated = c * 16 < p.rot_dim;
-  // the two 8-dim chunks of this thread
-  int d0 = c * 16, d1 = c * 16 + 8;
-  if (rotated && !p.interleaved) {
-    d0 = c * 8;
-    d1 = c * 8 + half;
-  }
+  const int d0 = rotated ? c * 8 : half + c * 8, d1 = d0 + (rotated ? half : D / 2 - half);
   uint4 x[HEADS][2];
 #pragma unroll
   for (int i = 0; i < HEADS; ++i) {
@@ -71,7 +65,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
     const float sign = p.inverse ? -p.scale : p.scale;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint64_t turns = p.turns[c * 8 + i] * n;
+      // pairs of the chunks: c * 8 + i, or four of each chunk
+      const int pair_at = p.interleaved ? (i < 4 ? d0 : d1) / 2 + (i & 3) : c * 8 + i;
+      const uint64_t turns = p.turns[pair_at] * n;
       const float a = static_cast<float>(static_cast<int32_t>(turns >> 32)) * 0x1p-32f;    // in [-1/2, 1/2]
       cs[i] = __builtin_amdgcn_cosf(a) * p.scale;
       sn[i] = __builtin_amdgcn_sinf(a) * sign;

@@ -33,7 +33,13 @@ class Case:
                                        i32(self.prefix, DEV), i32(self.window, DEV), self.block, mask_mode=mode, **kw)
 
     def want(self, mode="bidir", scale=None):
-        """Output, and A of the tolerance."""
+        """Output, and A of the tolerance (kept while the inputs stay the same)."""
+        key = (mode, scale, self.q.view(torch.int16).numpy().tobytes(), self.pool.k.numpy().tobytes())
+        if getattr(self, "_key", None) != key:
+            self._key, self._want = key, self._compute(mode, scale)
+        return self._want
+
+    def _compute(self, mode, scale):
         k, v = self.pool.values()
         m = oracle.MASK_BIDIR if mode == "bidir" else oracle.MASK_BLOCK_CAUSAL
         rest = self.pool.table, self.prefix, self.window, self.block, m, scale
@@ -55,9 +61,11 @@ def test_key_counts(gpu, keys, d, fmt):
     """Sequences that end at and around pages and tiles; NaN codes behind."""
     c = Case(keys, [keys - 1, max(keys - 2, 0), 0], [1, 1, 1], 1, 8, 2, d, fmt)
     c.check(c.run(gpu), what=f"{keys} keys")
-    c = Case(keys, [keys - min(keys, 16), 3], [min(keys, 16)] * 2, min(keys, 16), 4, 2, d, fmt)
-    for mode in ("bidir", "block_causal"):
-        c.check(c.run(gpu, mode), mode, what=f"{keys} keys, {mode}")
+    w = min(keys, 16)
+    for hq in (4, 8, 16, 32):                # units of 32 to 256 rows
+        c = Case(keys, [keys - w, 3], [w] * 2, w, hq, 2 if hq < 32 else 1, d, fmt)
+        for split in (0, 1 << 20):
+            c.check(c.run(gpu, kv_split_tokens=split), what=f"{keys} keys, {hq} heads, split {split}")
 
 
 @pytest.mark.parametrize("group,window,block", [(1, 1, 1), (1, 33, 33), (3, 11, 11), (4, 8, 4), (4, 9, 3), (4, 16, 16),
@@ -65,15 +73,18 @@ def test_key_counts(gpu, keys, d, fmt):
                                                 (4, 128, 32), (16, 8, 8), (1, 300, 50), (8, 65, 13)])
 @pytest.mark.parametrize("d", [64, 128])
 def test_row_counts(gpu, group, window, block, d):
-    """1 to 520 packed rows: part of a wave's rows, of a workgroup's, several."""
+    """1 to 520 packed rows: part of a wave's rows, of a workgroup's, several; in
+    the small units of short calls, and in the units that go by the rows (whole,
+    and cut)."""
     c = Case(group * window, [77, 600, 0], [window] * 3, block, 2 * group, 2, d)
-    for mode in ("bidir", "block_causal"):
-        c.check(c.run(gpu, mode), mode, what=mode)
+    for mode in ("bidir", "block_causal"):     # (units by split)
+        for split in (0, 1 << 20, 64):
+            c.check(c.run(gpu, mode, kv_split_tokens=split), mode, what=f"{mode}, split {split}")
 
 
 @pytest.mark.parametrize("split", [64, 128, 320, 1024])
 @pytest.mark.parametrize("mode", ["bidir", "block_causal"])
-@pytest.mark.parametrize("group,window", [(4, 1), (4, 12), (4, 32), (4, 72)])
+@pytest.mark.parametrize("group,window", [(4, 1), (4, 12), (4, 32), (4, 72), (8, 72)])
 def test_split_sequences(gpu, split, mode, group, window):
     """Units cut between many workgroups, ragged: several borders in one unit,
     several units in one share, windows of nothing between them."""
@@ -99,7 +110,8 @@ def test_sharp_rising_and_flat_scores(gpu, window):
     """Scores of hundreds, keys whose scores rise along the sequence (the
     reference maximum is raised again and again), equal scores, a zero q."""
     c = Case(3, [900], [window], window, 4, 1, 128, sigma_q=20.0, sigma_kv=3.0)
-    c.check(c.run(gpu), what="sharp")
+    for split in (0, 1 << 20, 128):
+        c.check(c.run(gpu, kv_split_tokens=split), what=f"sharp, split {split}")
     rng = np.random.default_rng(4)
     c = Case(4, [900], [window], window, 4, 1, 128)
     n = 900 + window
@@ -110,7 +122,8 @@ def test_sharp_rising_and_flat_scores(gpu, window):
     c.q = torch.full_like(c.q, 0.25)
     c.q[0, 1] = 0
     c.q[0, 2] = -0.25
-    c.check(c.run(gpu), what="rising")
+    for split in (0, 1 << 20, 128):
+        c.check(c.run(gpu, kv_split_tokens=split), what=f"rising, split {split}")
 
 
 def test_scales_far_apart(gpu):
@@ -130,13 +143,18 @@ def test_scales_far_apart(gpu):
     c.q[2, :, ::2] *= 2.0 ** -9            # values at both ends of a row's range
     c.check(c.run(gpu), what="scales")
     c.check(c.run(gpu, softmax_scale=0.5), scale=0.5, what="softmax scale")
+    for rows in (64, 256):                    # the kernels of larger units
+        c.q = c.q[:, :1].expand(4, rows // 4, 128).contiguous()
+        c.check(c.run(gpu, kv_split_tokens=1 << 20), what=f"scales, {rows} rows")
 
 
-def test_block_flags_and_gate(gpu):
-    """Only flagged blocks' rows are written; nothing is when the gate is 0."""
-    c = Case(6, [100, 2000], [32, 32], 8, 8, 2, 128)
+@pytest.mark.parametrize("heads", [2, 4, 8, 16])
+def test_block_flags_and_gate(gpu, heads):
+    """Only flagged blocks' rows are written; nothing is when the gate is 0.  (32
+    to 256 rows per KV head)"""
+    c = Case(6, [100, 2000], [32, 32], 8, heads, 2, 128)
     flags = torch.tensor([[1, 0, 0, 1], [0, 0, 0, 0]], dtype=torch.uint8, device=DEV)
-    for split in (0, 64):
+    for split in (0, 64, 1 << 20):
         out = torch.full(c.q.shape, 9.0, dtype=torch.bfloat16, device=DEV)
         c.run(gpu, "block_causal", out=out, block_flags=flags, kv_split_tokens=split)
         full = c.run(gpu, "block_causal", kv_split_tokens=split)
@@ -179,20 +197,24 @@ def test_bad_page_ids_are_clamped(gpu):
 
 
 def test_same_inputs_same_bits(gpu):
-    c = Case(9, [5000, 777, 3000], [32, 16, 8], 8, 16, 4, 128)
-    a = c.run(gpu, "block_causal")
-    for _ in range(3):
-        assert torch.equal(a, c.run(gpu, "block_causal"))
+    for heads, split in ((16, 0), (8, 64), (16, 64), (32, 128)):
+        c = Case(9, [5000, 777, 3000], [32, 16, 8], 8, heads, 4, 128)
+        a = c.run(gpu, "block_causal", kv_split_tokens=split)
+        for _ in range(3):
+            assert torch.equal(a, c.run(gpu, "block_causal", kv_split_tokens=split))
 
 
 def test_q_that_is_not_finite_stays_in_its_row(gpu):
     c = Case(10, [200], [4], 4, 4, 1, 128)
     c.q[1, 2, 5] = float("inf")
     c.q[3, 0, 0] = float("nan")
-    out = c.run(gpu).cpu()
     bad = torch.zeros(4, 4, dtype=torch.bool)
     bad[1, 2] = bad[3, 0] = True
-    assert bool(torch.isnan(out[bad]).all()) and bool(torch.isfinite(out[~bad]).all())
+    for rep in (1, 3, 16):                    # 16, 48 and 256 rows
+        q = c.q.repeat(1, rep, 1)
+        out = c.run(gpu, q=q.to(DEV), kv_split_tokens=0 if rep == 1 else 1 << 20).cpu()
+        b = bad.repeat(1, rep)
+        assert bool(torch.isnan(out[b]).all()) and bool(torch.isfinite(out[~b]).all())
 
 
 def test_pool_past_32_bits(gpu):
@@ -209,8 +231,8 @@ def test_pool_past_32_bits(gpu):
     small = [a[-64:].contiguous() for a in args]
     for a in (args, small):
         a[0], a[1] = a[0].view(torch.float8_e4m3fn), a[1].view(torch.float8_e4m3fn)
-    q = torch.randn(8, 32, d, generator=g, device=DEV, dtype=torch.bfloat16)
-    for split in (0, 64):
+    for heads, split in ((32, 0), (32, 64), (64, 64), (128, 64), (256, 128)):
+        q = torch.randn(8, heads, d, generator=g, device=DEV, dtype=torch.bfloat16)
         kw = dict(max_prefix_len=1016, max_window_len=8, kv_split_tokens=split)
         a = gpu.window_attention_q8(q, *args, table, i32([1016], DEV), i32([8], DEV), 8, **kw)
         b = gpu.window_attention_q8(q, *small, table - (pages - 64), i32([1016], DEV), i32([8], DEV), 8, **kw)
@@ -219,14 +241,14 @@ def test_pool_past_32_bits(gpu):
 
 def test_random_shapes(gpu):
     rng = np.random.default_rng(20)
-    for i in range(40):
+    for i in range(60):
         d, fmt = int(rng.choice([64, 128])), str(rng.choice(["e4m3", "e5m2"]))
         hkv, group = int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 4, 5, 8]))
         block = int(rng.choice([1, 3, 16, 32]))
         n = int(rng.integers(1, 6))
         win = (block * rng.integers(0, 5, n)).tolist()
         prefix = [int(x) for x in np.exp(rng.uniform(0, 8, n))]
-        split = int(rng.choice([0, 0, 64, 256]))
+        split = int(rng.choice([0, 64, 256, 1 << 20]))
         if sum(win) == 0:
             continue
         c = Case(100 + i, prefix, win, block, hkv * group, hkv, d, fmt, sigma_q=float(rng.choice([0.3, 1.0, 4.0])))
