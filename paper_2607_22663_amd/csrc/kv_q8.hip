@@ -327,7 +327,8 @@ __global__ __launch_bounds__(256) void kv_read_q8_kernel(KvQ8Params p) {
       uint4 w = {pair(f[0] * scale, f[1] * scale), pair(f[2] * scale, f[3] * scale), pair(f[4] * scale, f[5] * scale),
                  pair(f[6] * scale, f[7] * scale)};
       if (!valid) w = {0, 0, 0, 0};
-      *reinterpret_cast<uint4 *>(p.k_out + ((it.row + slot) * p.num_kv_heads + it.g) * D + (lane % kChunks) * 8) = w;
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), reinterpret_cast<u32x4 *>(p.k_out + ((it.row + slot) * p.num_kv_heads + it.g) * D + (lane % kChunks) * 8));
     }
   } else {
     const int tok0 = (lane / kPairs) * kTok;
@@ -346,7 +347,7 @@ __global__ __launch_bounds__(256) void kv_read_q8_kernel(KvQ8Params p) {
       const int slot = tok0 + i;
       if (slot < s0 || slot >= s1) continue;
       const uint32_t w = valid ? pair(f[0][i] * scale, f[1][i] * scale) : 0u;
-      *reinterpret_cast<uint32_t *>(p.v_out + ((it.row + slot) * p.num_kv_heads + it.g) * D + (lane % kPairs) * 2) = w;
+      __builtin_nontemporal_store(w, reinterpret_cast<uint32_t *>(p.v_out + ((it.row + slot) * p.num_kv_heads + it.g) * D + (lane % kPairs) * 2));
     }
   }
 }
