@@ -252,7 +252,7 @@ def _workspace(kind: str, device: torch.device, nbytes: int) -> Optional[torch.T
 MBE_ERR_WORKSPACE = 4
 
 
-def _call_with_workspace(call, size, opts, device, workspace, kind="attn"):
+def _call_with_workspace(call, size, opts, device, workspace):
     """Runs an attention call whose split plan may need a workspace.  With a
     caller's workspace, that one.  Otherwise the shared workspace of this
     stream as it is, first: only when the library reports it too small (or
@@ -263,7 +263,7 @@ def _call_with_workspace(call, size, opts, device, workspace, kind="attn"):
             raise ValueError("workspace must be a uint8 device tensor")
         opts.workspace, opts.workspace_bytes = _ptr(workspace), workspace.numel()
         return call()
-    key = (kind, device.index, opts.stream or 0)
+    key = ("attn", device.index, opts.stream or 0)
     ws = _workspaces.get(key)
     opts.workspace, opts.workspace_bytes = (_ptr(ws), ws.numel()) if ws is not None else (None, 0)
     status = call()
@@ -272,7 +272,7 @@ def _call_with_workspace(call, size, opts, device, workspace, kind="attn"):
     need = size()
     if need == ctypes.c_size_t(-1).value:
         return status
-    ws = _workspace(kind, device, need)
+    ws = _workspace("attn", device, need)
     opts.workspace, opts.workspace_bytes = (_ptr(ws), need) if ws is not None else (None, 0)
     return call()
 
@@ -815,7 +815,9 @@ def window_attention_q8(q, k_pages, v_pages, k_scales, v_scales, page_table, pre
     those of window_attention.  The lengths' bounds are needed on the host
     (max_prefix_len, max_window_len, or host copies of the lengths; without
     either the lengths are copied from the device, a synchronisation).  The work
-    is dealt out on the device by the true lengths."""
+    is dealt out on the device by the true lengths.  workspace: an optional uint8
+    device tensor of workspace_bytes_window_attention_q8 bytes; otherwise a call
+    that needs one takes memory of its own."""
     lib = load()
     kv = _pool_q8(k_pages, v_pages, k_scales, v_scales, page_table)
     index, dev = k_pages.get_device(), k_pages.device
@@ -863,10 +865,18 @@ def window_attention_q8(q, k_pages, v_pages, k_scales, v_scales, page_table, pre
     def call():
         return lib.mbe_window_attention_q8(*args)
 
-    def size():
-        return lib.mbe_window_attention_q8_workspace_size(ctypes.byref(kv), ctypes.byref(opts))
-
-    status = _call_with_workspace(call, size, opts, dev, workspace, "attn_q8")
+    if workspace is not None:
+        if workspace.dtype != torch.uint8 or workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous uint8 tensor on the pools' GPU")
+        opts.workspace, opts.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    status = call()
+    if status == MBE_ERR_WORKSPACE and workspace is None:
+        # memory of this call's own, from torch's allocator: calls on other streams
+        # and captured graphs never share it
+        need = lib.mbe_window_attention_q8_workspace_size(ctypes.byref(kv), ctypes.byref(opts))
+        own = torch.empty(need, dtype=torch.uint8, device=dev)
+        opts.workspace, opts.workspace_bytes = own.data_ptr(), need
+        status = call()
     if status:
         _check("mbe_window_attention_q8", status)
     return out

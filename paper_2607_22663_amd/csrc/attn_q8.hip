@@ -241,7 +241,8 @@ __device__ inline void leave_note(const AttnQ8Params &p, const Deal<ROWS> &d, co
 __device__ inline bool row_wanted(const AttnQ8Params &p, int b, int w, int row0, int r) {
   if (r >= w * p.group) return false;
   const int i = r / p.group;
-  if (static_cast<int64_t>(row0) + i >= p.total_q) return false;
+  const int64_t row = static_cast<int64_t>(row0) + i;
+  if (row < 0 || row >= p.total_q) return false;      // (lengths that do not fit the rows)
   return !p.block_flags || p.block_flags[static_cast<int64_t>(b) * p.flag_stride + i / p.block_size] != 0;
 }
 
