@@ -437,8 +437,11 @@ __device__ inline i32x8 operand(uint4 a, uint4 b) {
 // Units of 32 rows; the workgroup's four waves take key tiles in turn, each
 // straight from HBM into its registers, and join their results in LDS.  A tile's
 // K and V registers are loaded again for the wave's next tile right after their
-// last use, so that 8 to 16 KB a wave, and two workgroups on a CU, are always on
-// their way.
+// last use, so that 8 to 16 KB a wave are always on their way.  Bound by HBM (2 D
+// bytes a key, and few operations): one token of 32 sequences of 65536 keys, 4 KV
+// heads of 128 dims, 355 us, 6.05 TB/s; of 1000 to 8192 keys 34 us, 4.5 TB/s, of
+// which about 5 are the first loads' round trips (length, page, K) and the join in
+// LDS.
 constexpr int kStreamRows = 32;
 constexpr int kStreamWaves = 4;
 
@@ -636,7 +639,12 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void attn_q8_stream_kernel(At
 // A wave works on three (32-key block, row block) pairs at once: while the vector
 // unit turns one's scores into probabilities, the matrix unit multiplies the next
 // one's scores and adds P.V of the one before, all independent, instruction by
-// instruction in turn.
+// instruction in turn.  Blocks of 32 rows of 4 heads each (RG = 2) behind 8 x 16384
+// keys: 59 us with the join, 580 TFLOP/s; a tile takes 0.88 us.  Bound by what one
+// wave can issue: a vector instruction every 6 clocks where two waves of a SIMD
+// have one every 4, and a quarter of them move Q's operands, which the unified file
+// holds beyond its first 256 registers.  (The same units on waves of 32 rows over
+// tiles staged in LDS: 98 us where this form's first build took 74.)
 template <int D, int FMT, int RG>
 __global__ __launch_bounds__(256, 1) void attn_q8_wide_kernel(AttnQ8Params p) {
   constexpr int kRows = 64 * RG, KG = 4 / RG;
@@ -920,6 +928,11 @@ __global__ __launch_bounds__(256, 1) void attn_q8_wide_kernel(AttnQ8Params p) {
 // iteration t reads K of tiles t and t + 1 and V of t - 1 and t, from three LDS
 // buffers each; it writes K of t + 2 and V of t + 1 from registers, and loads K of
 // t + 4 and V of t + 3 into them: one barrier a tile, two tiles' time for a load.
+//
+// Windows of 128 rows of 4 heads behind 64 x 4096 to 32768 keys: 1.19 ms, 1.05
+// PFLOP/s, where a large bf16 product reaches 1.23 on this card.  A tile takes 1.46
+// us on one CU alone and 2.1 with all of them at work: bound by the matrix and
+// vector units at the clock that the board's power leaves (about 2.0 GHz).
 constexpr int kTileRows = 256, kTileThreads = 512;
 
 template <int D, int FMT>
@@ -1178,7 +1191,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_q8_tile_kernel(AttnQ8Par
 // ------------------------------------------------------------- the join
 // Workgroup x joins the unit that the note of share x + 1 names, if it names one.
 // A block takes RPB rows of it; a row's dims lie across D / 4 lanes, and its parts
-// are dealt to G groups of lanes, whose results meet in LDS.
+// are dealt to G groups of lanes, whose results meet in LDS.  Bound by the parts'
+// bytes where units are large (4 D per row and part: 67 MB in 11 us), by the chain
+// note -> statistics -> accumulators otherwise (4 us).
 template <int D, int ROWS, int RPB>
 __global__ __launch_bounds__(256) void attn_q8_join_kernel(AttnQ8Params p) {
   constexpr int kLanes = D / 4, G = 256 / (kLanes * RPB);
