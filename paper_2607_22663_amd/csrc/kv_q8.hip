@@ -18,7 +18,7 @@
 // Both calls move 6 bytes a value pair and are bound by HBM for long ranges, by
 // the chain lens -> page id -> scale for single tokens.  At 4 KV heads of 128 dims,
 // 79000 tokens of 32 sequences written in 50 us (4.9 TB/s, what a large copy
-// reaches), 151000 tokens read back in 80 us (5.6 TB/s); one token of each of 8
+// reaches), 151000 tokens read back in 84 us (5.6 TB/s); one token of each of 8
 // sequences written in 4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
