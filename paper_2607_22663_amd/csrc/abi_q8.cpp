@@ -195,18 +195,19 @@ mbe_status plan_attention(const mbe_paged_kv_q8 *kv, const mbe_attn_opts *o, int
   *pl = mbe::AttnQ8Plan{};
   const int64_t seq_rows = group * o->max_window_len;
   const int64_t tiles = (max_kv + mbe::kKeyTile - 1) / mbe::kKeyTile;
+  constexpr int64_t kCounted = 1LL << 32;       // (more than any call may have; times heads, within 64 bits)
   // units of `rows` rows within the bounds: no more than the rows fill
   auto units_of = [&](int64_t rows) {
     const int64_t each = (seq_rows + rows - 1) / rows;
     const int64_t all = std::min<int64_t>(o->batch * each, o->total_q * group / rows + o->batch);
-    return std::max<int64_t>(1, all * kv->num_kv_heads);
+    return std::max<int64_t>(1, std::min(all, kCounted) * kv->num_kv_heads);
   };
   const bool little = o->kv_split_tokens == 0 && units_of(32) <= kLittleWork / (tiles + kStartTiles);
   pl->rows = seq_rows <= 32 || little ? 32 : seq_rows <= 64 ? 64 : seq_rows <= 128 ? 128 : 256;
   const int form = pl->rows == 32 ? 0 : pl->rows <= 128 ? 1 : 2;
   const int64_t qtiles = (seq_rows + pl->rows - 1) / pl->rows;
   const int64_t units = units_of(pl->rows);
-  const int64_t grid = std::max<int64_t>(1, o->batch * qtiles * kv->num_kv_heads);
+  const int64_t grid = std::max<int64_t>(1, std::min(o->batch * qtiles, kCounted) * kv->num_kv_heads);
   pl->qtiles = static_cast<int32_t>(std::max<int64_t>(1, qtiles));
   pl->min_tiles = o->kv_split_tokens > 0 ? o->kv_split_tokens / mbe::kKeyTile : kMinTiles;
   // (the kernels count the tiles of all units in 32 bits, whatever the lengths within the bounds)

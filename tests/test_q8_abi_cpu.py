@@ -166,6 +166,9 @@ def test_attention_workspace(lib):
     assert 0 < size(batch=1024, max_prefix_len=1 << 20, total_q=1 << 18, **wide) < 1 << 28
     assert size(batch=1024, max_prefix_len=1 << 29, total_q=1 << 18, **wide) == 0      # (too many tiles to deal out)
     assert size(batch=1 << 30, max_prefix_len=1 << 29, total_q=2 ** 31 - 1, **wide) == bad
+    # (units whose number wraps to nothing in 64 bits)
+    assert size(_kv(num_kv_heads=4096), batch=1 << 30, num_q_heads=4096, max_prefix_len=0, max_window_len=1 << 30,
+                total_q=2 ** 31 - 1) == bad
     # the binding's query agrees
     q = torch.empty(64, 16, 128, device="meta")
     k = torch.empty(10, 4, 16, 128, dtype=torch.float8_e4m3fn, device="meta")
